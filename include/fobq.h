@@ -241,6 +241,118 @@ typedef struct {
 } fobq_layer;
 int fobq_quantize_layers_batched(fobq_ctx* ctx, int32_t n_layers, const fobq_layer* layers, const fobq_opts* opts);
 
+/* ---- running a quantized network -------------------------------------------
+ * A layer that has been quantized is run by products of its weights with activations; next to the weights a network
+ * that generates token by token reads its cache of keys and values.  The calls of this section hold both in few bits:
+ * matrices in 8-bit floating point with a scale for each block of 128 columns, and a cache on 4-bit grids.
+ * They only enqueue: they allocate nothing, wait for nothing, use no scratch of the context and no second stream, so they
+ * may be captured into a graph; every pointer inside a struct is device memory and must stay valid until the stream has
+ * reached the work, the structs themselves are host memory and may be released at once.  Where a call needs scratch
+ * the caller gives it (`work`; its size is asked for first), and two calls that may run at the same time, two captured
+ * graphs among them, need scratch of their own.  A layer that is enqueued on the context (fobq_quantize_layer_enqueue)
+ * does not disturb them.  Errors: EINVAL (a size, stride, type, alignment or pointer that a call does not take), EHIP.
+ * Calls with nothing to do (no rows, no outputs) succeed.  Rounding is to nearest, ties to even, everywhere. */
+typedef enum { FOBQ_F32 = 0, FOBQ_BF16 = 1, FOBQ_F16 = 2 } fobq_float;
+
+/* 8-bit floating point: e4m3 (4 exponent bits, largest value 448, no infinities), e5m2 (largest value 57344). */
+typedef enum { FOBQ_E4M3 = 0, FOBQ_E5M2 = 1 } fobq_fp8;
+
+/* A matrix in blocks of 128 consecutive columns and 1 or 128 consecutive rows; element (r, c) stands for
+ *   values[r * ld + c] * scales[(c / 128) * ld_scales + r / rows_per_scale].
+ * The last blocks may be partial.  values: 16-byte aligned, ld (bytes) a multiple of 16 and no less than cols; the calls
+ * that read a matrix may read each row, the last one too, up to the next multiple of 16 columns (and ignore what is there),
+ * those that write one leave what is behind column cols - 1 as it was.  1 <= rows, cols < 2^31 / 4 (0 allowed where nothing is read). */
+typedef struct {
+    void*   values;
+    float*  scales;
+    int64_t rows, cols, ld, ld_scales;   /* ld_scales >= ceil(rows / rows_per_scale)                     */
+    int32_t rows_per_scale;              /* 1 or 128                                                     */
+    int32_t format;                      /* fobq_fp8                                                     */
+} fobq_fp8_matrix;
+
+/* X (device, `type`, out->rows x out->cols, row stride ld >= cols elements) into out: per block
+ *   scale = max(max |x| / largest value of the format, 2^-126), value = x / scale rounded.
+ * A block that holds an Inf or NaN gets a NaN scale and NaN values. */
+int fobq_fp8_quantize(fobq_ctx* ctx, const void* X, int32_t type, int64_t ld, const fobq_fp8_matrix* out);
+
+/* A layer's codes, scales and zeros as fobq_quantize_layer returns them (dense, d_row x d_col and d_row x G, G = d_col /
+ * group or 1) as a matrix with rows_per_scale 1: value = code - zero, which e4m3 holds exactly for layers of up to 4 bits,
+ * scale = the grid's as returned.  The matrix stands for the layer's Q but for the rounding of the scales to fp32.  bits 2..4; out->format FOBQ_E4M3; group 0 or
+ * a multiple of 128 that divides d_col (EINVAL otherwise: a block has one scale). */
+int fobq_fp8_from_codes(fobq_ctx* ctx, const uint8_t* codes, const float* scales, const float* zeros, int32_t bits, int32_t group,
+                        const fobq_fp8_matrix* out);
+
+/* Y = A B^T: Y[m][n] = sum over columns of A's element (m, c) times B's element (n, c).  A: the activations, rows_per_scale 1;
+ * B: the weights, rows_per_scale 1 or 128, as many columns; the formats may differ.  Y: device, `type`, A->rows x B->rows, row
+ * stride ld >= B->rows elements.  Sums in fp32, rounded to `type` once; the same bits in every run on equal arguments.
+ * work: at least fobq_fp8_matmul_workspace's bytes (0: may be NULL), 16-byte aligned. */
+int fobq_fp8_matmul(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8_matrix* B, void* Y, int32_t type, int64_t ld,
+                    void* work, int64_t work_bytes);
+int fobq_fp8_matmul_workspace(fobq_ctx* ctx, int64_t m, int64_t n, int64_t k, int32_t type, int64_t* bytes);
+
+/* A cache of keys and values in 4 bits.  It has `pages` pages of `page_size` tokens (a power of two, 16 .. 4096) for each of
+ * `heads` heads; a token's head_dim (64, 128 or 256) channels of one head are a row on a grid of its own, the 4-bit grid
+ * of the layers with its scale rounded up to bf16:
+ *   lo = min(min x, 0), hi = max(max x, 0), scale = max((hi - lo) / 15 rounded up, 2^-126), zero = rint(-lo / scale),
+ *   code = clamp(rint(x / scale) + zero, 0, 15); channel c stands for scale * (code - zero).
+ * codes: pages x heads x page_size x head_dim / 2 bytes, channel 2 i in the lower half of byte i; grids: pages x heads x page_size
+ * words, the scale's 16 bits above, the zero point in the lowest four.  Both 16-byte aligned.  A row that holds an Inf or NaN (or
+ * whose range passes fp32) gets a NaN scale: it reads as NaN, and a query that sees it gets NaN. */
+typedef struct {
+    uint8_t*  k_codes;
+    uint8_t*  v_codes;
+    uint32_t* k_grids;
+    uint32_t* v_grids;
+    int64_t   pages;
+    int32_t   page_size, heads, head_dim, reserved;   /* reserved must be 0                              */
+} fobq_kv4_cache;
+
+/* Sequences of a call.  Sequence i owns the packed rows starts[i] .. starts[i + 1] - 1 (starts: n_seqs + 1 ascending entries in
+ * 0 .. rows; NULL: one row each, row i) and holds lengths[i] tokens, those of its rows included: they are its last ones, in order.
+ * Token t of it lies in page table[i * table_ld + t / page_size] at place t % page_size.  Rows behind the last
+ * sequence are not touched.  An entry outside 0 .. pages - 1 is no page: nothing is written there and its tokens are not there; so
+ * are tokens behind max_pages pages and rows whose token would come before token 0.  No address is formed from either. */
+typedef struct {
+    const int32_t* table;      /* device, n_seqs x max_pages, row stride table_ld                         */
+    const int32_t* lengths;    /* device, n_seqs                                                          */
+    const int32_t* starts;     /* device, n_seqs + 1, or NULL                                             */
+    int64_t rows;              /* packed rows of the call                                                 */
+    int64_t table_ld;
+    int32_t n_seqs, max_pages;
+} fobq_kv4_batch;
+
+/* New tokens into the cache: keys K and values V (device, BF16 or F16, rows x heads x head_dim; row and head strides in
+ * elements, channels adjacent).  No two rows of a call may have the same place. */
+int fobq_kv4_append(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv4_batch* batch, int32_t type, const void* K, int64_t k_row,
+                    int64_t k_head, const void* V, int64_t v_row, int64_t v_head);
+/* Back: what the rows' tokens stand for, into K and V (any type).  Tokens that are not there read 0. */
+int fobq_kv4_read(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv4_batch* batch, int32_t type, void* K, int64_t k_row,
+                  int64_t k_head, void* V, int64_t v_row, int64_t v_head);
+
+/* Attention of the batch's rows over their sequences' tokens in the cache: per row and query head h
+ *   out = sum_t p_t v_t,  p = softmax(scale * q . k_t) over the tokens t that the row sees, heads h / group of K and V.
+ * A row sees, causal != 0: the tokens up to its own; 0: all of its sequence; of those, window > 0: the last `window`.  A row that
+ * sees nothing is 0.  Scores, softmax and sums in fp32; the queries as given, the weights p in fp16 against the largest scale of the
+ * values met, the result rounded once.  The same bits in every run on equal arguments. */
+typedef struct {
+    const void* Q;             /* device, `type`, rows x (heads * group) x head_dim                       */
+    void*   out;               /* device, `type`, same shape                                              */
+    float*  lse;               /* device fp32 rows x (heads * group): log of the sum of exp(scores), or NULL */
+    int64_t q_row, q_head, out_row, out_head;   /* strides in elements                                    */
+    int64_t max_length;        /* most tokens that a sequence holds, as far as known (a hint for the launch; */
+                               /* longer sequences are still attended in full); 0: what the table can hold */
+    int32_t type;              /* FOBQ_BF16 or FOBQ_F16                                                   */
+    int32_t group;             /* query heads per head of the cache                                       */
+    int32_t causal, window;
+    float   scale;
+    int32_t reserved;          /* must be 0                                                               */
+} fobq_kv4_query;
+/* work: at least fobq_kv4_attention_workspace's bytes for the same cache, batch and query sizes (0: may be NULL), 16-byte aligned. */
+int fobq_kv4_attention(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv4_batch* batch, const fobq_kv4_query* query,
+                       void* work, int64_t work_bytes);
+int fobq_kv4_attention_workspace(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv4_batch* batch, const fobq_kv4_query* query,
+                                 int64_t* bytes);
+
 /* ---- stage-level entry points (test and benchmark hooks) ------------------ */
 
 /* Hinv = H^-1 for symmetric positive definite H via H = L L^T, L^-1, L^-T L^-1
@@ -330,8 +442,20 @@ int fobq_debug_offset_tables(int32_t k, int32_t pad, int64_t h, int64_t w, int32
  *   FOBQ_PLAN_HESSIAN  in: d_col, calibration columns of one fp64 accumulate call, from feature maps (0 / 1)
  *                  out: tile edge, slabs of an accumulation, slabs that this call can touch
  *   FOBQ_PLAN_SLABS  in: channels, kernel size of a stride-1 convolution, integer slices
- *                  out: slabs that fobq_hessian_begin reserves, slabs that its form by tap offsets takes (0: another form) */
-typedef enum { FOBQ_PLAN_PAD = 0, FOBQ_PLAN_ELIMINATE = 1, FOBQ_PLAN_HESSIAN = 2, FOBQ_PLAN_SLABS = 3 } fobq_plan;
+ *                  out: slabs that fobq_hessian_begin reserves, slabs that its form by tap offsets takes (0: another form)
+ *   FOBQ_PLAN_FP8_MATMUL  in: compute units, m, n, k, type of the result (fobq_float)
+ *                  out: rows of A and of B of a tile, parts of the contraction, blocks of 128 a part, bytes of work
+ *   FOBQ_PLAN_KV4_ATTENTION  in: compute units, head_dim, heads, group, n_seqs, rows, longest sequence
+ *                  out: query rows of a workgroup, whether its wavefronts share them, parts of the tokens, workgroups a head and part, bytes of work
+ *   FOBQ_PLAN_KV4_PLACE  in: page_size, pages, max_pages, n_seqs, rows, a packed row, then lengths (n_seqs), starts (n_seqs + 1), table (n_seqs x max_pages)
+ *                  out: the sequence, page and place that the row's token has (page -1: none)
+ *   FOBQ_PLAN_FP8_CHECK  in: rows, cols, ld, ld_scales, rows_per_scale, format, values, scales (addresses that are not followed)
+ *                  out: what a call says of such a matrix (fobq_status)
+ *   FOBQ_PLAN_KV4_CHECK  in: pages, page_size, heads, head_dim, reserved, n_seqs, rows, max_pages, table_ld, then addresses (not followed) of
+ *                  k_codes, v_codes, k_grids, v_grids, table, lengths
+ *                  out: what a call says of such a cache and batch (fobq_status) */
+typedef enum { FOBQ_PLAN_PAD = 0, FOBQ_PLAN_ELIMINATE = 1, FOBQ_PLAN_HESSIAN = 2, FOBQ_PLAN_SLABS = 3, FOBQ_PLAN_FP8_MATMUL = 4,
+               FOBQ_PLAN_KV4_ATTENTION = 5, FOBQ_PLAN_KV4_PLACE = 6, FOBQ_PLAN_FP8_CHECK = 7, FOBQ_PLAN_KV4_CHECK = 8 } fobq_plan;
 
 int fobq_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* out, int32_t n_out);
 

@@ -39,6 +39,28 @@ class FobqOut(ctypes.Structure):
                 ("Hinv_work", ctypes.c_void_p), ("loss", ctypes.c_void_p)]
 
 
+class FobqFp8Matrix(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("ld_scales", ctypes.c_int64), ("rows_per_scale", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class FobqKv4Cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_grids", ctypes.c_void_p), ("v_grids", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class FobqKv4Batch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("table_ld", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class FobqKv4Query(ctypes.Structure):
+    _fields_ = [("Q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
+                ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64), ("max_length", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
 class FobqLayer(ctypes.Structure):
     _fields_ = [("W", ctypes.c_void_p), ("d_row", ctypes.c_int64), ("d_col", ctypes.c_int64),
                 ("H", ctypes.c_void_p), ("out", FobqOut)]
@@ -81,6 +103,15 @@ def load_library() -> ctypes.CDLL:
     lib.fobq_workspace_bytes.argtypes = [vp, ctypes.POINTER(i64)]
     lib.fobq_hessian_form.argtypes = [vp, ctypes.POINTER(i32)]
     lib.fobq_obq_rows.argtypes = [vp, vp, i64, i64, vp, ctypes.POINTER(FobqOpts), i64, i64, vp, vp, vp, vp]
+    ptr = ctypes.POINTER
+    lib.fobq_fp8_quantize.argtypes = [vp, vp, i32, i64, ptr(FobqFp8Matrix)]
+    lib.fobq_fp8_from_codes.argtypes = [vp, vp, vp, vp, i32, i32, ptr(FobqFp8Matrix)]
+    lib.fobq_fp8_matmul.argtypes = [vp, ptr(FobqFp8Matrix), ptr(FobqFp8Matrix), vp, i32, i64, vp, i64]
+    lib.fobq_fp8_matmul_workspace.argtypes = [vp, i64, i64, i64, i32, ptr(i64)]
+    lib.fobq_kv4_append.argtypes = [vp, ptr(FobqKv4Cache), ptr(FobqKv4Batch), i32, vp, i64, i64, vp, i64, i64]
+    lib.fobq_kv4_read.argtypes = lib.fobq_kv4_append.argtypes
+    lib.fobq_kv4_attention.argtypes = [vp, ptr(FobqKv4Cache), ptr(FobqKv4Batch), ptr(FobqKv4Query), vp, i64]
+    lib.fobq_kv4_attention_workspace.argtypes = [vp, ptr(FobqKv4Cache), ptr(FobqKv4Batch), ptr(FobqKv4Query), ptr(i64)]
     lib.fobq_probe_int8_matrix_rate.argtypes = [vp, i32, ctypes.POINTER(dbl)]
     lib.fobq_profile_enable.argtypes = [vp, i32]
     lib.fobq_profile_get.argtypes = [vp, i32, ctypes.POINTER(dbl), ctypes.POINTER(i64)]
@@ -89,10 +120,17 @@ def load_library() -> ctypes.CDLL:
                  "fobq_hessian_accumulate_conv", "fobq_hessian_finalize", "fobq_quantize_layer",
                  "fobq_quantize_layer_enqueue", "fobq_quantize_layers_batched", "fobq_finish", "fobq_spd_inverse", "fobq_sensitivity",
                  "fobq_sensitivity_static", "fobq_debug_fail_after", "fobq_debug_wait_looks", "fobq_debug_plan", "fobq_debug_offset_tables", "fobq_workspace_bytes", "fobq_probe_int8_matrix_rate", "fobq_obq_rows", "fobq_hessian_form",
+                 "fobq_fp8_quantize", "fobq_fp8_from_codes", "fobq_fp8_matmul", "fobq_fp8_matmul_workspace",
+                 "fobq_kv4_append", "fobq_kv4_read", "fobq_kv4_attention", "fobq_kv4_attention_workspace",
                  "fobq_profile_enable", "fobq_profile_get", "fobq_profile_reset"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
+
+
+# fobq_float and fobq_fp8 by torch's names
+_FLOAT = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_FP8 = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
 
 
 class FobqError(RuntimeError):
@@ -109,6 +147,9 @@ def _ptr(t: Optional[torch.Tensor], dtype: torch.dtype, what: str) -> Optional[i
     return t.data_ptr()
 
 
+_streams = {}      # the device and the stream of every context made here
+
+
 # ---- functions with the names of the C entry points -------------------------------------------
 def fobq_create(device: int = 0, stream: Optional[int] = None) -> int:
     lib = load_library()
@@ -118,11 +159,13 @@ def fobq_create(device: int = 0, stream: Optional[int] = None) -> int:
     rc = lib.fobq_create(ctypes.byref(h), device, ctypes.c_void_p(stream))
     if rc != OK:
         raise FobqError(rc, "fobq_create failed")
+    _streams[h.value] = (device, stream)
     return h.value
 
 
 def fobq_destroy(ctx: int) -> None:
     load_library().fobq_destroy(ctypes.c_void_p(ctx))
+    _streams.pop(ctx, None)
 
 
 def fobq_last_error(ctx: int) -> str:
@@ -343,6 +386,7 @@ def fobq_debug_wait_looks(ctx: int, looks: int) -> None:
 
 
 PLAN_PAD, PLAN_ELIMINATE, PLAN_HESSIAN, PLAN_SLABS = 0, 1, 2, 3
+PLAN_FP8_MATMUL, PLAN_KV4_ATTENTION, PLAN_KV4_PLACE, PLAN_FP8_CHECK, PLAN_KV4_CHECK = 4, 5, 6, 7, 8
 
 
 def fobq_debug_plan(what: int, args, n_out: int):
@@ -375,6 +419,229 @@ def fobq_debug_offset_tables(k: int, pad: int, h: int, w: int):
     o += 4 * npair
     terms = [tuple(v[o + 2 * i:o + 2 * i + 2]) for i in range(nt)]
     return jobs, pairs, terms
+
+
+# ---- running a quantized network ----------------------------------------------------------------
+# Like the entry points they wrap, these calls enqueue on the context's stream and return.  What they allocate (outputs that are not
+# given, scratch) belongs to that stream; inputs that another stream made, and outputs that another stream uses, are ordered by the
+# caller, as between any two streams.  Under capture the context's stream has to be the captured one.
+def _need(t: torch.Tensor, ctx: int, dtypes, dims: int, what: str) -> torch.Tensor:
+    """A device tensor of one of these types whose last dimension is adjacent, on the context's device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        names = " or ".join(str(d) for d in dtypes)
+        got = f"{tuple(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise TypeError(f"{what}: need a {dims}-D device tensor of {names} with adjacent last dimension, got {got}")
+    home = _streams.get(ctx)
+    if home is not None and t.device.index != home[0]:
+        raise TypeError(f"{what}: on {t.device}, but the context is on device {home[0]}")
+    return t
+
+
+def _empty(ctx: int, shape, dtype: torch.dtype, device) -> torch.Tensor:
+    """Memory that belongs to the context's stream, which need not be the current one."""
+    home = _streams.get(ctx)
+    if home is None or torch.cuda.current_stream(device).cuda_stream == home[1]:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(home[1], device=device)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+@dataclass
+class Fp8Matrix:
+    """A matrix in 8-bit floating point: values (float8_e4m3fn or float8_e5m2, rows x cols, rows a multiple of 16 bytes apart) and the
+    scales (fp32, ceil(cols / 128) x ceil(rows / rows_per_scale)) of its blocks of 128 columns and 1 or 128 rows."""
+    values: torch.Tensor
+    scales: torch.Tensor
+    rows_per_scale: int = 1
+
+
+def _fp8(ctx: int, m: Fp8Matrix, what: str) -> FobqFp8Matrix:
+    v, s = _need(m.values, ctx, _FP8, 2, what + ".values"), _need(m.scales, ctx, (torch.float32,), 2, what + ".scales")
+    rows, cols = v.shape
+    per = m.rows_per_scale
+    wide = -(-cols // 16) * 16
+    if per not in (1, 128) or tuple(s.shape) != (-(-cols // 128), -(-rows // per)):
+        raise TypeError(f"{what}: rows_per_scale must be 1 or 128 and scales (ceil(cols / 128), ceil(rows / rows_per_scale)), "
+                        f"got {per} and {tuple(s.shape)} for {rows} x {cols}")
+    ld = v.stride(0) if rows > 1 and cols else wide
+    if rows and cols and v.storage_offset() + (rows - 1) * ld + wide > v.untyped_storage().nbytes():
+        raise TypeError(f"{what}: the last row must be readable to a multiple of 16 bytes")
+    return FobqFp8Matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, s.stride(0) if s.shape[0] > 1 else s.shape[1], per, _FP8[v.dtype])
+
+
+def _new_fp8(ctx: int, rows: int, cols: int, format: torch.dtype, per: int, device) -> Fp8Matrix:
+    if format not in _FP8 or per not in (1, 128):
+        raise TypeError(f"format must be float8_e4m3fn or float8_e5m2 and rows_per_scale 1 or 128, got {format} and {per}")
+    values = _empty(ctx, (rows, -(-cols // 16) * 16), format, device)
+    return Fp8Matrix(values if values.shape[1] == cols else values[:, :cols], _empty(ctx, (-(-cols // 128), -(-rows // per)), torch.float32, device), per)
+
+
+def fobq_fp8_quantize(ctx: int, X: torch.Tensor, format: torch.dtype = torch.float8_e4m3fn, rows_per_scale: int = 1,
+                      out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+    """X: 2-D device tensor (fp32, bf16 or fp16) -> Fp8Matrix: rows_per_scale 1 for activations, 1 or 128 for weights."""
+    _need(X, ctx, _FLOAT, 2, "X")
+    rows, cols = X.shape
+    if out is None:
+        out = _new_fp8(ctx, rows, cols, format, rows_per_scale, X.device)
+    m = _fp8(ctx, out, "out")
+    if (m.rows, m.cols) != (rows, cols):
+        raise TypeError(f"out is {m.rows} x {m.cols}, X {rows} x {cols}")
+    _check(ctx, load_library().fobq_fp8_quantize(ctx, X.data_ptr(), _FLOAT[X.dtype], X.stride(0) if rows > 1 else cols, ctypes.byref(m)))
+    return out
+
+
+def fobq_fp8_from_codes(ctx: int, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int = 4,
+                        out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+    """A layer quantized to up to 4 bits (LayerOutput's codes, scales, zeros; one grid per row, or groups of a multiple of 128 columns)
+    as an Fp8Matrix that stands for its Q (but for the rounding of the returned scales to fp32)."""
+    _need(codes, ctx, (torch.uint8,), 2, "codes")
+    rows, cols = codes.shape
+    for name, t in (("scales", scales), ("zeros", zeros)):
+        _need(t, ctx, (torch.float32,), 2, name)
+        if t.shape != scales.shape or t.shape[0] != rows or t.shape[1] < 1 or cols % t.shape[1] or not t.is_contiguous():
+            raise TypeError(f"{name}: need contiguous rows x groups, got {tuple(t.shape)} for codes {rows} x {cols}")
+    if not codes.is_contiguous():
+        raise TypeError("codes: need a contiguous tensor")
+    if out is None:
+        out = _new_fp8(ctx, rows, cols, torch.float8_e4m3fn, 1, codes.device)
+    m = _fp8(ctx, out, "out")
+    if (m.rows, m.cols) != (rows, cols):
+        raise TypeError(f"out is {m.rows} x {m.cols}, codes {rows} x {cols}")
+    group = cols // scales.shape[1] if scales.shape[1] > 1 else 0
+    _check(ctx, load_library().fobq_fp8_from_codes(ctx, codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), bits, group, ctypes.byref(m)))
+    return out
+
+
+def _scratch(ctx: int, need: int, device) -> Optional[torch.Tensor]:
+    return _empty(ctx, (need,), torch.uint8, device) if need else None
+
+
+def fobq_fp8_matmul(ctx: int, A: Fp8Matrix, B: Fp8Matrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """A (activations, m x k) times B (weights, n x k) transposed -> m x n of `dtype` (fp32, bf16 or fp16), or into `out`."""
+    a, b = _fp8(ctx, A, "A"), _fp8(ctx, B, "B")
+    if a.cols != b.cols:
+        raise TypeError(f"A has {a.cols} columns, B {b.cols}")
+    device = A.values.device
+    if out is None:
+        if dtype not in _FLOAT:
+            raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+        out = _empty(ctx, (a.rows, b.rows), dtype, device)
+    else:
+        _need(out, ctx, _FLOAT, 2, "out")
+        if tuple(out.shape) != (a.rows, b.rows):
+            raise TypeError(f"out: need {a.rows} x {b.rows}, got {tuple(out.shape)}")
+    lib, need = load_library(), ctypes.c_int64(0)
+    _check(ctx, lib.fobq_fp8_matmul_workspace(ctx, a.rows, b.rows, a.cols, _FLOAT[out.dtype], ctypes.byref(need)))
+    work = _scratch(ctx, need.value, device)
+    _check(ctx, lib.fobq_fp8_matmul(ctx, ctypes.byref(a), ctypes.byref(b), out.data_ptr(), _FLOAT[out.dtype], out.stride(0) if a.rows > 1 else b.rows,
+                                    work.data_ptr() if work is not None else None, need.value))
+    return out
+
+
+@dataclass
+class Kv4Cache:
+    """A cache of keys and values in 4 bits: codes (uint8, pages x heads x page_size x head_dim / 2) and grid words (int32, pages x heads
+    x page_size), contiguous."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_grids: torch.Tensor
+    v_grids: torch.Tensor
+
+    @staticmethod
+    def empty(pages: int, heads: int, head_dim: int, page_size: int = 64, device="cuda") -> "Kv4Cache":
+        codes = [torch.empty((pages, heads, page_size, head_dim // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+        return Kv4Cache(*codes, *[torch.empty((pages, heads, page_size), dtype=torch.int32, device=device) for _ in range(2)])
+
+
+@dataclass
+class Kv4Batch:
+    """The sequences of a call: table (int32, n_seqs x max_pages: page numbers), lengths (int32, n_seqs: tokens held, new ones included)
+    and starts (int32, n_seqs + 1: the sequences' packed rows; None: one row each)."""
+    table: torch.Tensor
+    lengths: torch.Tensor
+    starts: Optional[torch.Tensor] = None
+
+
+def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
+    k = _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
+    shape = k.shape
+    for name in ("k_codes", "v_codes", "k_grids", "v_grids"):
+        t = getattr(cache, name)
+        if name != "k_codes":
+            _need(t, ctx, (torch.uint8,) if "codes" in name else (torch.int32,), 4 if "codes" in name else 3, name)
+        if t.shape != (shape if "codes" in name else shape[:3]) or not t.is_contiguous():
+            raise TypeError(f"{name}: need a contiguous {tuple(shape if 'codes' in name else shape[:3])}, got {tuple(t.shape)}")
+    table, lengths = _need(batch.table, ctx, (torch.int32,), 2, "table"), _need(batch.lengths, ctx, (torch.int32,), 1, "lengths")
+    n, width = table.shape
+    if lengths.shape[0] != n:
+        raise TypeError(f"lengths: need {n} entries, got {lengths.shape[0]}")
+    starts = batch.starts
+    if starts is not None and _need(starts, ctx, (torch.int32,), 1, "starts").shape[0] != n + 1:
+        raise TypeError(f"starts: need {n + 1} entries, got {starts.shape[0]}")
+    c = FobqKv4Cache(k.data_ptr(), cache.v_codes.data_ptr(), cache.k_grids.data_ptr(), cache.v_grids.data_ptr(), shape[0], shape[2], shape[1], 2 * shape[3], 0)
+    b = FobqKv4Batch(table.data_ptr(), lengths.data_ptr(), starts.data_ptr() if starts is not None else None, rows,
+                     table.stride(0) if n > 1 else width, n, width)
+    return c, b
+
+
+def _kv_rows(ctx: int, cache: Kv4Cache, k: torch.Tensor, v: torch.Tensor, dtypes):
+    _need(k, ctx, dtypes, 3, "k")
+    _need(v, ctx, dtypes, 3, "v")
+    if k.shape != v.shape or k.dtype != v.dtype or tuple(k.shape[1:]) != (cache.k_codes.shape[1], 2 * cache.k_codes.shape[3]):
+        raise TypeError(f"k and v: need rows x {cache.k_codes.shape[1]} x {2 * cache.k_codes.shape[3]} of one type, got {tuple(k.shape)} {k.dtype} "
+                        f"and {tuple(v.shape)} {v.dtype}")
+    return (_FLOAT[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1))
+
+
+def fobq_kv4_append(ctx: int, cache: Kv4Cache, batch: Kv4Batch, k: torch.Tensor, v: torch.Tensor) -> None:
+    """New keys and values (bf16 or fp16, rows x heads x head_dim, any row and head strides) into the sequences' last places."""
+    _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
+    args = _kv_rows(ctx, cache, k, v, (torch.bfloat16, torch.float16))
+    c, b = _kv4(ctx, cache, batch, k.shape[0])
+    _check(ctx, load_library().fobq_kv4_append(ctx, ctypes.byref(c), ctypes.byref(b), *args))
+
+
+def fobq_kv4_read(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int, dtype: torch.dtype = torch.bfloat16, out=None):
+    """What the packed rows' places in the cache stand for: (k, v), rows x heads x head_dim of `dtype`, or into out = (k, v)."""
+    _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
+    if out is None:
+        if dtype not in _FLOAT:
+            raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+        shape = (rows, cache.k_codes.shape[1], 2 * cache.k_codes.shape[3])
+        out = tuple(_empty(ctx, shape, dtype, cache.k_codes.device) for _ in range(2))
+    k, v = out
+    args = _kv_rows(ctx, cache, k, v, tuple(_FLOAT))
+    if k.shape[0] != rows:
+        raise TypeError(f"out: need {rows} rows, got {k.shape[0]}")
+    c, b = _kv4(ctx, cache, batch, rows)
+    _check(ctx, load_library().fobq_kv4_read(ctx, ctypes.byref(c), ctypes.byref(b), *args))
+    return k, v
+
+
+def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tensor, *, scale: Optional[float] = None, causal: bool = True,
+                       window: int = 0, max_length: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q (bf16 or fp16, rows x query heads x head_dim) over the sequences' tokens -> the same shape, or into `out`.  scale: head_dim^-0.5
+    unless given.  max_length: the most tokens a sequence holds, if known (a hint).  lse (fp32, rows x query heads): filled."""
+    _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
+    _need(q, ctx, (torch.bfloat16, torch.float16), 3, "q")
+    rows, heads_q, dim = q.shape
+    heads = cache.k_codes.shape[1]
+    if dim != 2 * cache.k_codes.shape[3] or heads < 1 or heads_q < 1 or heads_q % heads:
+        raise TypeError(f"q: need rows x (a multiple of {heads}) x {2 * cache.k_codes.shape[3]}, got {tuple(q.shape)}")
+    if out is None:
+        out = _empty(ctx, (rows, heads_q, dim), q.dtype, q.device)
+    elif _need(out, ctx, (q.dtype,), 3, "out").shape != q.shape:
+        raise TypeError(f"out: need {tuple(q.shape)}, got {tuple(out.shape)}")
+    if lse is not None and (tuple(_need(lse, ctx, (torch.float32,), 2, "lse").shape) != (rows, heads_q) or not lse.is_contiguous()):
+        raise TypeError(f"lse: need a contiguous {(rows, heads_q)}, got {tuple(lse.shape)}")
+    c, b = _kv4(ctx, cache, batch, rows)
+    d = FobqKv4Query(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+                     max_length, _FLOAT[q.dtype], heads_q // heads, int(causal), window, dim ** -0.5 if scale is None else scale, 0)
+    lib, need = load_library(), ctypes.c_int64(0)
+    _check(ctx, lib.fobq_kv4_attention_workspace(ctx, ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), ctypes.byref(need)))
+    work = _scratch(ctx, need.value, q.device)
+    _check(ctx, lib.fobq_kv4_attention(ctx, ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), work.data_ptr() if work is not None else None, need.value))
+    return out
 
 
 def FOBQ_PROFILE_STAGE(stage: int) -> int:
@@ -449,6 +716,24 @@ class Ctx:
 
     def finish(self) -> None:
         fobq_finish(self.handle)
+
+    def fp8_quantize(self, X: torch.Tensor, format: torch.dtype = torch.float8_e4m3fn, rows_per_scale: int = 1, out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+        return fobq_fp8_quantize(self.handle, X, format, rows_per_scale, out)
+
+    def fp8_from_codes(self, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int = 4, out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+        return fobq_fp8_from_codes(self.handle, codes, scales, zeros, bits, out)
+
+    def fp8_matmul(self, A: Fp8Matrix, B: Fp8Matrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return fobq_fp8_matmul(self.handle, A, B, dtype, out)
+
+    def kv4_append(self, cache: Kv4Cache, batch: Kv4Batch, k: torch.Tensor, v: torch.Tensor) -> None:
+        fobq_kv4_append(self.handle, cache, batch, k, v)
+
+    def kv4_read(self, cache: Kv4Cache, batch: Kv4Batch, rows: int, dtype: torch.dtype = torch.bfloat16, out=None):
+        return fobq_kv4_read(self.handle, cache, batch, rows, dtype, out)
+
+    def kv4_attention(self, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tensor, **kw) -> torch.Tensor:
+        return fobq_kv4_attention(self.handle, cache, batch, q, **kw)
 
     def workspace_bytes(self) -> int:
         return fobq_workspace_bytes(self.handle)

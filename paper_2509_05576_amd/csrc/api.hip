@@ -86,16 +86,6 @@ static void fold_events(fobq_ctx* c)
     }
 }
 
-// `ctx->fail_countdown` (test hook, fobq_debug_fail_after): the n-th check from now reports a failure
-// without the HIP call having failed, so that the error paths can be exercised from the host.
-#define FOBQ_TRY(expr, what)                                                              \
-    do {                                                                                  \
-        hipError_t e__ = (expr);                                                          \
-        if (e__ != hipSuccess) return hip_err(ctx, e__, what);                            \
-        if (ctx->fail_countdown > 0 && --ctx->fail_countdown == 0)                        \
-            return set_err(ctx, FOBQ_EHIP, "%s: injected failure (test hook)", what);     \
-    } while (0)
-
 // the side stream and the events (no timing) that order it behind the context's stream and back; made once
 static hipError_t ensure_side_stream(fobq_ctx* c)
 {
@@ -139,17 +129,6 @@ static void make_side_for_later(fobq_ctx* c)
     if (ensure_side_stream(c) != hipSuccess || ensure_sync_event(c, EV_FORK) != hipSuccess || ensure_sync_event(c, EV_JOIN) != hipSuccess)
         (void)hipGetLastError();             // nothing depends on it
 }
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-        if (prev != dev) ok = (hipSetDevice(dev) == hipSuccess);
-    }
-    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
-};
 
 constexpr int64_t MAX_DCOL = 32768;
 constexpr int64_t MAX_DROW = 65535;
@@ -994,7 +973,7 @@ int fobq_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* out,
         for (int l = 0; l < n; ++l) { out[4 * l] = p[l].nr; out[4 * l + 1] = p[l].n1; out[4 * l + 2] = p[l].n2; out[4 * l + 3] = p[l].n3; }
         return FOBQ_OK;
     }
-    return FOBQ_EINVAL;
+    return lowbit_debug_plan(what, in, n_in, out, n_out);
 }
 
 int fobq_debug_fail_after(fobq_ctx* ctx, int n)

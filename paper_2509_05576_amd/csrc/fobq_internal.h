@@ -203,8 +203,32 @@ struct BatchLayer {
 constexpr int BATCH_MAX_D = 256;      // columns of a layer in a batched call (4 panels of 64)
 constexpr int BATCH_MAX_LAYERS = 256;
 
+// api_lowbit.hip: the plans of fobq_debug_plan that belong there
+int lowbit_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* out, int32_t n_out);
+
 int set_err(fobq_ctx* c, int code, const char* fmt, ...);
 int hip_err(fobq_ctx* c, hipError_t e, const char* what);
+
+// `ctx->fail_countdown` (test hook, fobq_debug_fail_after): the n-th check from now reports a failure
+// without the HIP call having failed, so that the error paths can be exercised from the host.
+#define FOBQ_TRY(expr, what)                                                              \
+    do {                                                                                  \
+        hipError_t e__ = (expr);                                                          \
+        if (e__ != hipSuccess) return hip_err(ctx, e__, what);                            \
+        if (ctx->fail_countdown > 0 && --ctx->fail_countdown == 0)                        \
+            return set_err(ctx, FOBQ_EHIP, "%s: injected failure (test hook)", what);     \
+    } while (0)
+
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = true;
+    explicit DeviceGuard(int dev)
+    {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        if (prev != dev) ok = (hipSetDevice(dev) == hipSuccess);
+    }
+    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
+};
 
 // Timing of a stage that is exactly one launch: the two events ride on the launch as its start and stop
 // events (no bubble on the stream; StageScope's records cost about 4 us each).  Both null when the stage is

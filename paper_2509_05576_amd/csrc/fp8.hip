@@ -1,0 +1,185 @@
+// Matrices in 8-bit floating point with a scale for each block of 128 columns and 1 or 128 rows: from 16- and 32-bit matrices, and
+// from the codes of a quantized layer.
+//
+// A block's scale is its largest magnitude over the type's largest value (e4m3 448, e5m2 57344), at least 2^-126 (which a block of
+// zeros has); the values are the nearest ones to x / scale, ties to even.  A block that holds an Inf or NaN is NaN throughout.
+// The quotient: with top = 0.875 * 2^9 or * 2^16, x / (most / top) = (0.875 x) / (most / 2^9 or 2^16), whose operands are exact for 16-bit x;
+// one multiplication by the reciprocal and one correction from the remainder round it as a division would, so that a quotient on the border
+// of two 8-bit values is seen as one.  It never passes the largest value by more than a rounding, which the conversion takes back.
+#include "lowbit.h"
+
+namespace fobq {
+
+constexpr float FP8_TINY = 1.17549435e-38f;
+
+template <int FORMAT> struct Fp8;          // fobq_fp8
+template <> struct Fp8<FOBQ_E4M3> { static constexpr float TOP = 448.f, POW = 1.f / 512; };
+template <> struct Fp8<FOBQ_E5M2> { static constexpr float TOP = 57344.f, POW = 1.f / 65536; };
+
+template <int FORMAT>
+__device__ __forceinline__ uint32_t to_fp8x4(float a, float b, float c, float d)
+{
+    int w = 0;
+    if constexpr (FORMAT == FOBQ_E4M3) {
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    } else {
+        w = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, w, false);
+        w = __builtin_amdgcn_cvt_pk_bf8_f32(c, d, w, true);
+    }
+    return (uint32_t)w;
+}
+
+// what turns a block's values into 8-bit ones
+struct Fp8Scale { float scale, pre, most, inv, corr; };
+template <int FORMAT>
+__device__ __forceinline__ Fp8Scale fp8_scale(uint32_t bits)
+{
+    const float most = __uint_as_float(bits), scale = most / Fp8<FORMAT>::TOP;
+    if (bits >= 0x7f800000u) return Fp8Scale{__builtin_nanf(""), __builtin_nanf(""), 0.f, 1.f, 0.f};
+    if (scale < FP8_TINY) return Fp8Scale{FP8_TINY, 1.f, 0.f, 0x1p126f, 0.f};
+    const float m = most * Fp8<FORMAT>::POW, inv = 1.f / m;
+    return Fp8Scale{scale, 0.875f, m, inv, inv};
+}
+// x / scale
+__device__ __forceinline__ float fp8_quotient(const Fp8Scale& s, float x)
+{
+    const float t = x * s.pre, y = t * s.inv;
+    return fmaf(fmaf(-y, s.most, t), s.corr, y);
+}
+
+// 8 values into 8 bytes of a row, or those of them that the row has
+template <int FORMAT>
+__device__ __forceinline__ void put8(uint8_t* __restrict__ dst, int left, const Fp8Scale& s, const float* x)
+{
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fp8_quotient(s, x[i]);
+    const uint32_t w[2] = {to_fp8x4<FORMAT>(y[0], y[1], y[2], y[3]), to_fp8x4<FORMAT>(y[4], y[5], y[6], y[7])};
+    if (left >= 8) __builtin_memcpy(dst, w, 8);
+    else
+        for (int i = 0; i < left; ++i) dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+}
+template <class T>
+__device__ __forceinline__ void get8(const T* __restrict__ src, int left, float* x)
+{
+    if (left >= 8) { load8(src, x); return; }
+    for (int i = 0; i < 8; ++i) x[i] = i < left ? (float)src[i] : 0.f;
+}
+// the largest magnitude as its bits, which order as the magnitudes do, Inf and NaN above all others
+__device__ __forceinline__ uint32_t most8(const float* x)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    return m;
+}
+__device__ __forceinline__ uint32_t other(uint32_t m, int off) { return (uint32_t)__shfl_xor((int)m, off); }
+
+// A scale per row: 16 lanes have a block, 8 columns each; a wavefront four consecutive blocks of a row.
+template <class T, int FORMAT>
+__global__ __launch_bounds__(256) void fp8_rows_kernel(const T* __restrict__ x, int64_t ld, Fp8View out)
+{
+    const int lane = threadIdx.x & 63;
+    const int blocks = (out.cols + 127) / 128, quads = (blocks + 3) / 4;
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t row = item / quads;
+    const int col = (int)(item - row * quads) * 512 + 8 * lane, left = out.cols - col;
+    if (row >= out.rows) return;
+    float v[8];
+    get8(x + row * ld + col, left, v);
+    uint32_t most = most8(v);
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) most = max(most, other(most, off));
+    const Fp8Scale s = fp8_scale<FORMAT>(most);
+    put8<FORMAT>(out.values + row * out.ld + col, left, s, v);
+    if ((lane & 15) == 0 && left > 0) out.scales[(int64_t)(col / 128) * out.ld_scales + row] = s.scale;
+}
+
+// A scale per 128 rows: a workgroup has a block of 128 x 128, 64 values a thread, which stay in registers between the two passes.
+template <class T, int FORMAT>
+__global__ __launch_bounds__(256) void fp8_tiles_kernel(const T* __restrict__ x, int64_t ld, Fp8View out)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int col = blockIdx.x * 128 + 8 * (tid & 15), left = out.cols - col;
+    const int64_t row0 = (int64_t)blockIdx.y * 128 + (tid >> 4);
+    __shared__ uint32_t part[4];
+    float v[8][8];
+    uint32_t most = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t row = row0 + 16 * k;
+        get8(x + row * ld + col, row < out.rows ? left : 0, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = max(most, most8(v[k]));
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) most = max(most, other(most, off));
+    if (lane == 0) part[tid >> 6] = most;
+    __syncthreads();
+    most = max(max(part[0], part[1]), max(part[2], part[3]));
+    const Fp8Scale s = fp8_scale<FORMAT>(most);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int64_t row = row0 + 16 * k;
+        if (row < out.rows) put8<FORMAT>(out.values + row * out.ld + col, left, s, v[k]);
+    }
+    if (tid == 0) out.scales[(int64_t)blockIdx.x * out.ld_scales + blockIdx.y] = s.scale;
+}
+
+// The codes of a layer (Section 3: q = scale (code - zero)): code - zero is an integer of at most 15 in magnitude for codes of up to
+// four bits, which e4m3 holds exactly, and the grid's scale is the block's.  16 codes a thread.
+__global__ __launch_bounds__(256) void fp8_codes_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales, const float* __restrict__ zeros,
+                                                        int groups, int group, Fp8View out)
+{
+    const int pieces = (out.cols + 15) / 16;
+    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = item / pieces;
+    const int col = (int)(item - row * pieces) * 16, left = out.cols - col;
+    if (row >= out.rows) return;
+    const int64_t g = row * groups + (group ? col / group : 0);
+    const float zero = zeros[g];
+    if (col % 128 == 0) out.scales[(int64_t)(col / 128) * out.ld_scales + row] = scales[g];
+    const uint8_t* __restrict__ src = codes + row * out.cols + col;
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (left >= 16) __builtin_memcpy(w, src, 16);
+    else
+        for (int i = 0; i < left; ++i) w[i >> 2] |= (uint32_t)src[i] << (8 * (i & 3));
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        w[k] = to_fp8x4<FOBQ_E4M3>((float)(w[k] & 255u) - zero, (float)(w[k] >> 8 & 255u) - zero, (float)(w[k] >> 16 & 255u) - zero, (float)(w[k] >> 24) - zero);
+    uint8_t* dst = out.values + row * out.ld + col;
+    if (left >= 16) __builtin_memcpy(dst, w, 16);
+    else
+        for (int i = 0; i < left; ++i) dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+}
+
+template <class T, int FORMAT>
+static hipError_t quantize_of(hipStream_t s, const void* x, int64_t ld, const Fp8View& out)
+{
+    const int blocks = (out.cols + 127) / 128;
+    if (out.per == 1) {
+        const int64_t items = (int64_t)out.rows * ((blocks + 3) / 4);
+        hipLaunchKernelGGL((fp8_rows_kernel<T, FORMAT>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, static_cast<const T*>(x), ld, out);
+    } else {
+        hipLaunchKernelGGL((fp8_tiles_kernel<T, FORMAT>), dim3((unsigned)blocks, (unsigned)((out.rows + 127) / 128)), dim3(256), 0, s, static_cast<const T*>(x), ld, out);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_fp8_quantize(hipStream_t s, const void* x, int type, int64_t ld, const Fp8View& out)
+{
+    const bool e4 = out.format == FOBQ_E4M3;
+    if (type == FOBQ_F32) return e4 ? quantize_of<float, FOBQ_E4M3>(s, x, ld, out) : quantize_of<float, FOBQ_E5M2>(s, x, ld, out);
+    if (type == FOBQ_BF16) return e4 ? quantize_of<bf16_t, FOBQ_E4M3>(s, x, ld, out) : quantize_of<bf16_t, FOBQ_E5M2>(s, x, ld, out);
+    return e4 ? quantize_of<f16_t, FOBQ_E4M3>(s, x, ld, out) : quantize_of<f16_t, FOBQ_E5M2>(s, x, ld, out);
+}
+
+hipError_t launch_fp8_from_codes(hipStream_t s, const uint8_t* codes, const float* scales, const float* zeros, int group, const Fp8View& out)
+{
+    const int64_t items = (int64_t)out.rows * ((out.cols + 15) / 16);
+    hipLaunchKernelGGL(fp8_codes_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, codes, scales, zeros, group ? out.cols / group : 1, group, out);
+    return hipGetLastError();
+}
+
+}  // namespace fobq

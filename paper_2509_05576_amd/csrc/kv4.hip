@@ -1,0 +1,146 @@
+// Rows of the 4-bit cache: new keys and values onto their grids (append) and back (read).
+//
+// Every row of a head's `dim` channels has a grid of 16 levels of its own, the layers' min-max grid at 4 bits (Section 3): lo =
+// min(min x, 0), hi = max(max x, 0), scale = (hi - lo) / 15, zero = rint(-lo / scale), code = clamp(rint(x / scale) + zero, 0, 15).
+// The scale is held in bf16 and rounded up to it, so that 15 steps still reach from lo to hi, and codes and zero are taken against
+// the scale as held.  All quotients are correctly rounded: the inputs have at most 11 bits and the scale 8, so that a quotient that
+// is not on the border of two levels is at least 2^-20 away from it, and the fp32 one falls on the same side as the exact one.
+//
+// Memory bound: a lane has 8 channels of a row, 16 bytes in, one word of codes out; dim / 8 lanes share a row and its minimum and
+// maximum by shuffles.
+#include "kv4.h"
+
+namespace fobq {
+
+constexpr float KV4_TINY = 1.17549435e-38f;   // 2^-126: the smallest scale, and what a row of zeros gets
+
+// where packed row `row` of head h lies in the cache, as a row number, or -1
+__device__ __forceinline__ int64_t kv4_row_of(const Kv4View& c, const Kv4Seqs& s, int row, int h)
+{
+    const int b = s.starts ? wave_search(s.n_seqs, row, [&](int i) { return (int64_t)kv4_rows(s.starts, i, s.rows).first; }) : row;
+    // several sequences may begin at this row: the last of them has it, the others are empty
+    const Kv4Place p = kv4_place(s, c.pages, c.shift, b, row);
+    return p.page < 0 ? -1 : (((int64_t)p.page * c.heads + h) << c.shift) + p.place;
+}
+
+// One wavefront per packed row: its lanes go through the heads' rows of keys (blockIdx.y = 0) or values, 64 / (dim / 8) at a time.
+template <class T, int DIM>
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4View c, Kv4Seqs s, const T* __restrict__ k, int64_t k_row, int64_t k_head,
+                                                         const T* __restrict__ v, int64_t v_row, int64_t v_head)
+{
+    constexpr int LANES = DIM / 8, AT_ONCE = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (row >= s.rows) return;
+    const bool values = blockIdx.y != 0;
+    const int64_t first = kv4_row_of(c, s, row, 0);
+    if (first < 0) return;
+    const T* __restrict__ src = values ? v + (int64_t)row * v_row : k + (int64_t)row * k_row;
+    const int64_t head_ld = values ? v_head : k_head;
+    uint8_t* __restrict__ codes = values ? c.v_codes : c.k_codes;
+    uint32_t* __restrict__ grids = values ? c.v_grids : c.k_grids;
+    const int part = lane % LANES;
+    for (int h0 = 0; h0 < c.heads; h0 += AT_ONCE) {
+        const int h = h0 + lane / LANES;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (h < c.heads) load8(src + h * head_ld + 8 * part, x);
+        float lo = 0.f, hi = 0.f, bad = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            lo = fminf(lo, x[i]);
+            hi = fmaxf(hi, x[i]);
+            bad = fmaf(x[i], 0.f, bad);          // NaN as soon as one of them is not finite
+        }
+#pragma unroll
+        for (int off = LANES / 2; off > 0; off >>= 1) {
+            lo = fminf(lo, __shfl_xor(lo, off));
+            hi = fmaxf(hi, __shfl_xor(hi, off));
+            bad += __shfl_xor(bad, off);
+        }
+        if (h >= c.heads) continue;
+        const float r = (hi - lo) / 15.f;
+        float scale = __uint_as_float((__float_as_uint(r) + 0xffffu) & 0xffff0000u);
+        scale = fmaxf(scale, KV4_TINY);
+        uint32_t word = 0;
+        uint32_t grid = 0x7fc00000u;             // a row that is not finite, or whose range is not: NaN throughout
+        if (bad == 0.f && r <= 3.4028235e38f) {
+            const float zero = fminf(fmaxf(rintf(-lo / scale), 0.f), 15.f);
+            grid = __float_as_uint(scale) | (uint32_t)zero;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = fminf(fmaxf(rintf(x[i] / scale) + zero, 0.f), 15.f);
+                word |= (uint32_t)q << (4 * i);
+            }
+        }
+        const int64_t at = first + ((int64_t)h << c.shift);
+        *reinterpret_cast<uint32_t*>(codes + at * (DIM / 2) + 4 * part) = word;
+        if (part == 0) grids[at] = grid;
+    }
+}
+
+// The same rows back as the values they stand for, scale * (code - zero), rounded to T once.  Tokens on no page of the cache read 0.
+template <class T, int DIM>
+__global__ __launch_bounds__(256) void kv4_read_kernel(Kv4View c, Kv4Seqs s, T* __restrict__ k, int64_t k_row, int64_t k_head,
+                                                       T* __restrict__ v, int64_t v_row, int64_t v_head)
+{
+    constexpr int LANES = DIM / 8, AT_ONCE = 64 / LANES;
+    const int lane = threadIdx.x & 63;
+    const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (row >= s.rows || (s.starts && row >= kv4_rows(s.starts, s.n_seqs - 1, s.rows).first + kv4_rows(s.starts, s.n_seqs - 1, s.rows).count)) return;
+    const bool values = blockIdx.y != 0;
+    const int64_t first = kv4_row_of(c, s, row, 0);
+    T* __restrict__ dst = values ? v + (int64_t)row * v_row : k + (int64_t)row * k_row;
+    const int64_t head_ld = values ? v_head : k_head;
+    const uint8_t* __restrict__ codes = values ? c.v_codes : c.k_codes;
+    const uint32_t* __restrict__ grids = values ? c.v_grids : c.k_grids;
+    const int part = lane % LANES;
+    for (int h = lane / LANES; h < c.heads; h += AT_ONCE) {
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (first >= 0) {
+            const int64_t at = first + ((int64_t)h << c.shift);
+            const uint32_t word = *reinterpret_cast<const uint32_t*>(codes + at * (DIM / 2) + 4 * part), grid = grids[at];
+            const float scale = __uint_as_float(grid & 0xffff0000u), zero = (float)kv4_zero(grid);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = scale * ((float)(word >> (4 * i) & 15u) - zero);
+        }
+        store8(dst + h * head_ld + 8 * part, x);
+    }
+}
+
+template <class T>
+static hipError_t append_of(hipStream_t st, const Kv4View& c, const Kv4Seqs& s, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
+                            int64_t v_head)
+{
+    const dim3 grid((unsigned)((s.rows + 3) / 4), 2), block(256);
+    const T *kt = static_cast<const T*>(k), *vt = static_cast<const T*>(v);
+    if (c.dim == 64) hipLaunchKernelGGL((kv4_append_kernel<T, 64>), grid, block, 0, st, c, s, kt, k_row, k_head, vt, v_row, v_head);
+    else if (c.dim == 128) hipLaunchKernelGGL((kv4_append_kernel<T, 128>), grid, block, 0, st, c, s, kt, k_row, k_head, vt, v_row, v_head);
+    else hipLaunchKernelGGL((kv4_append_kernel<T, 256>), grid, block, 0, st, c, s, kt, k_row, k_head, vt, v_row, v_head);
+    return hipGetLastError();
+}
+
+template <class T>
+static hipError_t read_of(hipStream_t st, const Kv4View& c, const Kv4Seqs& s, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row, int64_t v_head)
+{
+    const dim3 grid((unsigned)((s.rows + 3) / 4), 2), block(256);
+    T *kt = static_cast<T*>(k), *vt = static_cast<T*>(v);
+    if (c.dim == 64) hipLaunchKernelGGL((kv4_read_kernel<T, 64>), grid, block, 0, st, c, s, kt, k_row, k_head, vt, v_row, v_head);
+    else if (c.dim == 128) hipLaunchKernelGGL((kv4_read_kernel<T, 128>), grid, block, 0, st, c, s, kt, k_row, k_head, vt, v_row, v_head);
+    else hipLaunchKernelGGL((kv4_read_kernel<T, 256>), grid, block, 0, st, c, s, kt, k_row, k_head, vt, v_row, v_head);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv4_append(hipStream_t st, const Kv4View& c, const Kv4Seqs& s, int type, const void* k, int64_t k_row, int64_t k_head, const void* v,
+                             int64_t v_row, int64_t v_head)
+{
+    return type == FOBQ_BF16 ? append_of<bf16_t>(st, c, s, k, k_row, k_head, v, v_row, v_head) : append_of<f16_t>(st, c, s, k, k_row, k_head, v, v_row, v_head);
+}
+
+hipError_t launch_kv4_read(hipStream_t st, const Kv4View& c, const Kv4Seqs& s, int type, void* k, int64_t k_row, int64_t k_head, void* v, int64_t v_row,
+                           int64_t v_head)
+{
+    if (type == FOBQ_F32) return read_of<float>(st, c, s, k, k_row, k_head, v, v_row, v_head);
+    return type == FOBQ_BF16 ? read_of<bf16_t>(st, c, s, k, k_row, k_head, v, v_row, v_head) : read_of<f16_t>(st, c, s, k, k_row, k_head, v, v_row, v_head);
+}
+
+}  // namespace fobq
