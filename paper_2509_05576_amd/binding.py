@@ -131,6 +131,7 @@ def load_library() -> ctypes.CDLL:
 # fobq_float and fobq_fp8 by torch's names
 _FLOAT = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _FP8 = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+_F32, _U8, _I32, _HALF = (torch.float32,), (torch.uint8,), (torch.int32,), (torch.bfloat16, torch.float16)
 
 
 class FobqError(RuntimeError):
@@ -425,14 +426,19 @@ def fobq_debug_offset_tables(k: int, pad: int, h: int, w: int):
 # Like the entry points they wrap, these calls enqueue on the context's stream and return.  What they allocate (outputs that are not
 # given, scratch) belongs to that stream; inputs that another stream made, and outputs that another stream uses, are ordered by the
 # caller, as between any two streams.  Under capture the context's stream has to be the captured one.
+# The checks of a call are a few attribute reads each: a call takes the host 3 us to launch, and a step of generation makes hundreds.
+_current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)      # (the public call makes a stream object: 1.9 us against 0.1)
+
+
 def _need(t: torch.Tensor, ctx: int, dtypes, dims: int, what: str) -> torch.Tensor:
     """A device tensor of one of these types whose last dimension is adjacent, on the context's device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
         names = " or ".join(str(d) for d in dtypes)
         got = f"{tuple(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise TypeError(f"{what}: need a {dims}-D device tensor of {names} with adjacent last dimension, got {got}")
     home = _streams.get(ctx)
-    if home is not None and t.device.index != home[0]:
+    if home is not None and t.get_device() != home[0]:
         raise TypeError(f"{what}: on {t.device}, but the context is on device {home[0]}")
     return t
 
@@ -440,7 +446,7 @@ def _need(t: torch.Tensor, ctx: int, dtypes, dims: int, what: str) -> torch.Tens
 def _empty(ctx: int, shape, dtype: torch.dtype, device) -> torch.Tensor:
     """Memory that belongs to the context's stream, which need not be the current one."""
     home = _streams.get(ctx)
-    if home is None or torch.cuda.current_stream(device).cuda_stream == home[1]:
+    if home is None or _current_stream(device.index) == home[1]:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(torch.cuda.ExternalStream(home[1], device=device)):
         return torch.empty(shape, dtype=dtype, device=device)
@@ -456,24 +462,35 @@ class Fp8Matrix:
 
 
 def _fp8(ctx: int, m: Fp8Matrix, what: str) -> FobqFp8Matrix:
-    v, s = _need(m.values, ctx, _FP8, 2, what + ".values"), _need(m.scales, ctx, (torch.float32,), 2, what + ".scales")
-    rows, cols = v.shape
-    per = m.rows_per_scale
-    wide = -(-cols // 16) * 16
-    if per not in (1, 128) or tuple(s.shape) != (-(-cols // 128), -(-rows // per)):
+    v, s, per = _need(m.values, ctx, _FP8, 2, what + ".values"), _need(m.scales, ctx, _F32, 2, what + ".scales"), m.rows_per_scale
+    (rows, cols), (sc, sr) = v.shape, s.shape
+    wide = (cols + 15) & -16
+    if per not in (1, 128) or sc != (cols + 127) // 128 or sr != (rows + per - 1) // per:
         raise TypeError(f"{what}: rows_per_scale must be 1 or 128 and scales (ceil(cols / 128), ceil(rows / rows_per_scale)), "
-                        f"got {per} and {tuple(s.shape)} for {rows} x {cols}")
+                        f"got {per} and {(sc, sr)} for {rows} x {cols}")
     ld = v.stride(0) if rows > 1 and cols else wide
-    if rows and cols and v.storage_offset() + (rows - 1) * ld + wide > v.untyped_storage().nbytes():
+    if wide != cols and rows and v.storage_offset() + (rows - 1) * ld + wide > v.untyped_storage().nbytes():
         raise TypeError(f"{what}: the last row must be readable to a multiple of 16 bytes")
-    return FobqFp8Matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, s.stride(0) if s.shape[0] > 1 else s.shape[1], per, _FP8[v.dtype])
+    return FobqFp8Matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, s.stride(0) if sc > 1 else sr, per, _FP8[v.dtype])
 
 
-def _new_fp8(ctx: int, rows: int, cols: int, format: torch.dtype, per: int, device) -> Fp8Matrix:
+def _new_fp8(ctx: int, rows: int, cols: int, format: torch.dtype, per: int, device):
+    """A new matrix, and what the library calls it."""
     if format not in _FP8 or per not in (1, 128):
         raise TypeError(f"format must be float8_e4m3fn or float8_e5m2 and rows_per_scale 1 or 128, got {format} and {per}")
-    values = _empty(ctx, (rows, -(-cols // 16) * 16), format, device)
-    return Fp8Matrix(values if values.shape[1] == cols else values[:, :cols], _empty(ctx, (-(-cols // 128), -(-rows // per)), torch.float32, device), per)
+    wide, sr = (cols + 15) & -16, (rows + per - 1) // per
+    values, scales = _empty(ctx, (rows, wide), format, device), _empty(ctx, ((cols + 127) // 128, sr), torch.float32, device)
+    return (Fp8Matrix(values if wide == cols else values[:, :cols], scales, per),
+            FobqFp8Matrix(values.data_ptr(), scales.data_ptr(), rows, cols, wide, sr, per, _FP8[format]))
+
+
+def _out_fp8(ctx: int, out: Optional[Fp8Matrix], rows: int, cols: int, format: torch.dtype, per: int, device):
+    if out is None:
+        return _new_fp8(ctx, rows, cols, format, per, device)
+    m = _fp8(ctx, out, "out")
+    if m.rows != rows or m.cols != cols:
+        raise TypeError(f"out is {m.rows} x {m.cols}, need {rows} x {cols}")
+    return out, m
 
 
 def fobq_fp8_quantize(ctx: int, X: torch.Tensor, format: torch.dtype = torch.float8_e4m3fn, rows_per_scale: int = 1,
@@ -481,11 +498,7 @@ def fobq_fp8_quantize(ctx: int, X: torch.Tensor, format: torch.dtype = torch.flo
     """X: 2-D device tensor (fp32, bf16 or fp16) -> Fp8Matrix: rows_per_scale 1 for activations, 1 or 128 for weights."""
     _need(X, ctx, _FLOAT, 2, "X")
     rows, cols = X.shape
-    if out is None:
-        out = _new_fp8(ctx, rows, cols, format, rows_per_scale, X.device)
-    m = _fp8(ctx, out, "out")
-    if (m.rows, m.cols) != (rows, cols):
-        raise TypeError(f"out is {m.rows} x {m.cols}, X {rows} x {cols}")
+    out, m = _out_fp8(ctx, out, rows, cols, format, rows_per_scale, X.device)
     _check(ctx, load_library().fobq_fp8_quantize(ctx, X.data_ptr(), _FLOAT[X.dtype], X.stride(0) if rows > 1 else cols, ctypes.byref(m)))
     return out
 
@@ -497,16 +510,12 @@ def fobq_fp8_from_codes(ctx: int, codes: torch.Tensor, scales: torch.Tensor, zer
     _need(codes, ctx, (torch.uint8,), 2, "codes")
     rows, cols = codes.shape
     for name, t in (("scales", scales), ("zeros", zeros)):
-        _need(t, ctx, (torch.float32,), 2, name)
+        _need(t, ctx, _F32, 2, name)
         if t.shape != scales.shape or t.shape[0] != rows or t.shape[1] < 1 or cols % t.shape[1] or not t.is_contiguous():
             raise TypeError(f"{name}: need contiguous rows x groups, got {tuple(t.shape)} for codes {rows} x {cols}")
     if not codes.is_contiguous():
         raise TypeError("codes: need a contiguous tensor")
-    if out is None:
-        out = _new_fp8(ctx, rows, cols, torch.float8_e4m3fn, 1, codes.device)
-    m = _fp8(ctx, out, "out")
-    if (m.rows, m.cols) != (rows, cols):
-        raise TypeError(f"out is {m.rows} x {m.cols}, codes {rows} x {cols}")
+    out, m = _out_fp8(ctx, out, rows, cols, torch.float8_e4m3fn, 1, codes.device)
     group = cols // scales.shape[1] if scales.shape[1] > 1 else 0
     _check(ctx, load_library().fobq_fp8_from_codes(ctx, codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), bits, group, ctypes.byref(m)))
     return out
@@ -563,57 +572,52 @@ class Kv4Batch:
 
 
 def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
-    k = _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
+    """What the library calls a cache and a batch."""
+    k, v = _need(cache.k_codes, ctx, _U8, 4, "k_codes"), _need(cache.v_codes, ctx, _U8, 4, "v_codes")
+    kg, vg = _need(cache.k_grids, ctx, _I32, 3, "k_grids"), _need(cache.v_grids, ctx, _I32, 3, "v_grids")
     shape = k.shape
-    for name in ("k_codes", "v_codes", "k_grids", "v_grids"):
-        t = getattr(cache, name)
-        if name != "k_codes":
-            _need(t, ctx, (torch.uint8,) if "codes" in name else (torch.int32,), 4 if "codes" in name else 3, name)
-        if t.shape != (shape if "codes" in name else shape[:3]) or not t.is_contiguous():
-            raise TypeError(f"{name}: need a contiguous {tuple(shape if 'codes' in name else shape[:3])}, got {tuple(t.shape)}")
-    table, lengths = _need(batch.table, ctx, (torch.int32,), 2, "table"), _need(batch.lengths, ctx, (torch.int32,), 1, "lengths")
+    pages, heads, page, half = shape
+    if v.shape != shape or kg.shape != shape[:3] or vg.shape != shape[:3] or not (
+            k.is_contiguous() and v.is_contiguous() and kg.is_contiguous() and vg.is_contiguous()):
+        raise TypeError(f"cache: need contiguous codes {tuple(shape)} and grids {tuple(shape[:3])}, got v_codes {tuple(v.shape)}, "
+                        f"k_grids {tuple(kg.shape)}, v_grids {tuple(vg.shape)}")
+    table, lengths, starts = _need(batch.table, ctx, _I32, 2, "table"), _need(batch.lengths, ctx, _I32, 1, "lengths"), batch.starts
     n, width = table.shape
     if lengths.shape[0] != n:
         raise TypeError(f"lengths: need {n} entries, got {lengths.shape[0]}")
-    starts = batch.starts
-    if starts is not None and _need(starts, ctx, (torch.int32,), 1, "starts").shape[0] != n + 1:
+    if starts is not None and _need(starts, ctx, _I32, 1, "starts").shape[0] != n + 1:
         raise TypeError(f"starts: need {n + 1} entries, got {starts.shape[0]}")
-    c = FobqKv4Cache(k.data_ptr(), cache.v_codes.data_ptr(), cache.k_grids.data_ptr(), cache.v_grids.data_ptr(), shape[0], shape[2], shape[1], 2 * shape[3], 0)
-    b = FobqKv4Batch(table.data_ptr(), lengths.data_ptr(), starts.data_ptr() if starts is not None else None, rows,
-                     table.stride(0) if n > 1 else width, n, width)
-    return c, b
+    return (FobqKv4Cache(k.data_ptr(), v.data_ptr(), kg.data_ptr(), vg.data_ptr(), pages, page, heads, 2 * half, 0),
+            FobqKv4Batch(table.data_ptr(), lengths.data_ptr(), starts.data_ptr() if starts is not None else None, rows,
+                         table.stride(0) if n > 1 else width, n, width))
 
 
-def _kv_rows(ctx: int, cache: Kv4Cache, k: torch.Tensor, v: torch.Tensor, dtypes):
+def _kv_rows(ctx: int, c: FobqKv4Cache, k: torch.Tensor, v: torch.Tensor, rows: int, dtypes):
     _need(k, ctx, dtypes, 3, "k")
     _need(v, ctx, dtypes, 3, "v")
-    if k.shape != v.shape or k.dtype != v.dtype or tuple(k.shape[1:]) != (cache.k_codes.shape[1], 2 * cache.k_codes.shape[3]):
-        raise TypeError(f"k and v: need rows x {cache.k_codes.shape[1]} x {2 * cache.k_codes.shape[3]} of one type, got {tuple(k.shape)} {k.dtype} "
-                        f"and {tuple(v.shape)} {v.dtype}")
+    shape = k.shape
+    if v.shape != shape or k.dtype != v.dtype or shape[0] != rows or shape[1] != c.heads or shape[2] != c.head_dim:
+        raise TypeError(f"k and v: need {(rows, c.heads, c.head_dim)} of one type, got {tuple(shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
     return (_FLOAT[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1))
 
 
 def fobq_kv4_append(ctx: int, cache: Kv4Cache, batch: Kv4Batch, k: torch.Tensor, v: torch.Tensor) -> None:
     """New keys and values (bf16 or fp16, rows x heads x head_dim, any row and head strides) into the sequences' last places."""
-    _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
-    args = _kv_rows(ctx, cache, k, v, (torch.bfloat16, torch.float16))
     c, b = _kv4(ctx, cache, batch, k.shape[0])
+    args = _kv_rows(ctx, c, k, v, b.rows, _HALF)
     _check(ctx, load_library().fobq_kv4_append(ctx, ctypes.byref(c), ctypes.byref(b), *args))
 
 
 def fobq_kv4_read(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int, dtype: torch.dtype = torch.bfloat16, out=None):
     """What the packed rows' places in the cache stand for: (k, v), rows x heads x head_dim of `dtype`, or into out = (k, v)."""
-    _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
+    c, b = _kv4(ctx, cache, batch, rows)
     if out is None:
         if dtype not in _FLOAT:
             raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        shape = (rows, cache.k_codes.shape[1], 2 * cache.k_codes.shape[3])
-        out = tuple(_empty(ctx, shape, dtype, cache.k_codes.device) for _ in range(2))
+        shape, device = (rows, c.heads, c.head_dim), cache.k_codes.device
+        out = (_empty(ctx, shape, dtype, device), _empty(ctx, shape, dtype, device))
     k, v = out
-    args = _kv_rows(ctx, cache, k, v, tuple(_FLOAT))
-    if k.shape[0] != rows:
-        raise TypeError(f"out: need {rows} rows, got {k.shape[0]}")
-    c, b = _kv4(ctx, cache, batch, rows)
+    args = _kv_rows(ctx, c, k, v, rows, _FLOAT)
     _check(ctx, load_library().fobq_kv4_read(ctx, ctypes.byref(c), ctypes.byref(b), *args))
     return k, v
 
@@ -622,19 +626,18 @@ def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tens
                        window: int = 0, max_length: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q (bf16 or fp16, rows x query heads x head_dim) over the sequences' tokens -> the same shape, or into `out`.  scale: head_dim^-0.5
     unless given.  max_length: the most tokens a sequence holds, if known (a hint).  lse (fp32, rows x query heads): filled."""
-    _need(cache.k_codes, ctx, (torch.uint8,), 4, "k_codes")
-    _need(q, ctx, (torch.bfloat16, torch.float16), 3, "q")
+    _need(q, ctx, _HALF, 3, "q")
     rows, heads_q, dim = q.shape
-    heads = cache.k_codes.shape[1]
-    if dim != 2 * cache.k_codes.shape[3] or heads < 1 or heads_q < 1 or heads_q % heads:
-        raise TypeError(f"q: need rows x (a multiple of {heads}) x {2 * cache.k_codes.shape[3]}, got {tuple(q.shape)}")
+    c, b = _kv4(ctx, cache, batch, rows)
+    heads = c.heads
+    if dim != c.head_dim or heads < 1 or heads_q < 1 or heads_q % heads:
+        raise TypeError(f"q: need rows x (a multiple of {heads}) x {c.head_dim}, got {tuple(q.shape)}")
     if out is None:
         out = _empty(ctx, (rows, heads_q, dim), q.dtype, q.device)
     elif _need(out, ctx, (q.dtype,), 3, "out").shape != q.shape:
         raise TypeError(f"out: need {tuple(q.shape)}, got {tuple(out.shape)}")
-    if lse is not None and (tuple(_need(lse, ctx, (torch.float32,), 2, "lse").shape) != (rows, heads_q) or not lse.is_contiguous()):
+    if lse is not None and (tuple(_need(lse, ctx, _F32, 2, "lse").shape) != (rows, heads_q) or not lse.is_contiguous()):
         raise TypeError(f"lse: need a contiguous {(rows, heads_q)}, got {tuple(lse.shape)}")
-    c, b = _kv4(ctx, cache, batch, rows)
     d = FobqKv4Query(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q.stride(0), q.stride(1), out.stride(0), out.stride(1),
                      max_length, _FLOAT[q.dtype], heads_q // heads, int(causal), window, dim ** -0.5 if scale is None else scale, 0)
     lib, need = load_library(), ctypes.c_int64(0)

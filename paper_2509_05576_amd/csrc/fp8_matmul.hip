@@ -88,7 +88,11 @@ __device__ __forceinline__ void put4(const MatmulArgs& g, int part, int m, int n
     if (g.parts > 1) {
         float* dst = g.work + ((int64_t)part * g.a.rows + m) * g.b.rows + n;
         if (left >= 4) __builtin_memcpy(dst, &v, 16);
-        else for (int i = 0; i < left; ++i) dst[i] = v[i];
+        else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < left) dst[i] = v[i];
+        }
         return;
     }
     auto out = [&](auto zero) {
@@ -98,7 +102,11 @@ __device__ __forceinline__ void put4(const MatmulArgs& g, int part, int m, int n
 #pragma unroll
         for (int i = 0; i < 4; ++i) t[i] = (T)v[i];
         if (left >= 4) __builtin_memcpy(dst, t, sizeof t);
-        else for (int i = 0; i < left; ++i) dst[i] = t[i];
+        else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < left) dst[i] = t[i];
+        }
     };
     if (g.type == FOBQ_F32) out(0.f);
     else if (g.type == FOBQ_BF16) out((bf16_t)0.f);
@@ -221,7 +229,11 @@ __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(MatmulArgs g)
     for (int p = 0; p < g.parts; ++p, src += (int64_t)g.a.rows * g.b.rows) {
         f4 v = {0.f, 0.f, 0.f, 0.f};
         if (left >= 4) __builtin_memcpy(&v, src, 16);
-        else for (int i = 0; i < left; ++i) v[i] = src[i];
+        else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < left) v[i] = src[i];
+        }
         sum += v;
     }
     MatmulArgs whole = g;

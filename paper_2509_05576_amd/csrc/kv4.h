@@ -11,11 +11,12 @@ __host__ __device__ inline uint32_t kv4_zero(uint32_t word) { return word & 15u;
 
 // The page that holds token t of a sequence, or -1: behind the table, or an entry that is no page of the cache.  No kernel forms an
 // address from an entry that did not pass here.
-__host__ __device__ inline int kv4_page(const int32_t* row, int max_pages, int pages, int shift, int64_t t)
+__host__ __device__ inline int kv4_page(const int32_t* row, int max_pages, int pages, int shift, int t)
 {
-    if (t < 0 || (t >> shift) >= max_pages) return -1;
-    const int page = row[t >> shift];
-    return page >= 0 && page < pages ? page : -1;
+    const unsigned at = (unsigned)t >> shift;       // (a negative t is far behind any table)
+    if (at >= (unsigned)max_pages) return -1;
+    const int page = row[at];
+    return (unsigned)page < (unsigned)pages ? page : -1;
 }
 
 // Sequence b of packed rows has rows [first, first + count): starts as the caller gave them, kept inside 0 .. rows.
@@ -42,8 +43,9 @@ __host__ __device__ inline Kv4Place kv4_place(const Kv4Seqs& s, int pages, int s
 {
     const Kv4Rows r = kv4_rows(s.starts, b, s.rows);
     if (row < r.first || row >= r.first + r.count) return Kv4Place{-1, 0};
-    const int64_t t = (int64_t)kv4_length(s.lengths, b, s.max_pages, shift) - r.count + (row - r.first);
-    return Kv4Place{kv4_page(s.table + (int64_t)b * s.table_ld, s.max_pages, pages, shift, t), (int)(t & ((1 << shift) - 1))};
+    const int t = kv4_length(s.lengths, b, s.max_pages, shift) - r.count + (row - r.first);
+    if (t < 0) return Kv4Place{-1, 0};
+    return Kv4Place{kv4_page(s.table + (int64_t)b * s.table_ld, s.max_pages, pages, shift, t), t & ((1 << shift) - 1)};
 }
 
 #ifdef __HIPCC__

@@ -45,6 +45,19 @@ struct AttnArgs {
     float* part_ml;        // the same without dim: maximum (in binary orders) and sum
 };
 
+// (x & mask) | bits is one instruction where the compiler has the mask in a scalar register and the bits in a vector one; as two
+// literals they cost an instruction each.  So the bits are made where it cannot see what they are.  (The instruction itself is left to the
+// compiler: between it and a matrix instruction that reads its result there have to be wait states, which inline asm does not get.)
+struct Bits { uint32_t b128, h1024, h64; };
+__device__ __forceinline__ Bits offset_bits()
+{
+    Bits b{0x43004300u, 0x64006400u, 0x54005400u};
+    asm("" : "+v"(b.b128), "+v"(b.h1024), "+v"(b.h64));
+    return b;
+}
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t bits) { return (x & mask) | bits; }
+constexpr uint32_t LOW = 0x000f000fu, HIGH = 0x00f000f0u;
+
 template <class T> struct Frag;
 template <> struct Frag<bf16_t> {
     static __device__ __forceinline__ f4 mfma(u4 a, u4 b, f4 c)
@@ -53,11 +66,11 @@ template <> struct Frag<bf16_t> {
     }
     static constexpr float OFFSET = 128.f;
     // 8 codes as 128 + code: register j has codes j and j + 4
-    static __device__ __forceinline__ u4 codes(uint32_t w)
+    static __device__ __forceinline__ u4 codes(uint32_t w, const Bits& b)
     {
         u4 r;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = (w >> (4 * j) & 0x000f000fu) | 0x43004300u;
+        for (int j = 0; j < 4; ++j) r[j] = and_or(w >> (4 * j), LOW, b.b128);
         return r;
     }
 };
@@ -68,95 +81,188 @@ template <> struct Frag<f16_t> {
     }
     static constexpr float OFFSET = 0.f;
     // 8 codes as they are
-    static __device__ __forceinline__ u4 codes(uint32_t w)
+    static __device__ __forceinline__ u4 codes(uint32_t w, const Bits& b)
     {
         u4 r;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t x = j < 2 ? w : w >> 8;
-            const h2 low = __builtin_bit_cast(h2, (x & 0x000f000fu) | 0x64006400u), high = __builtin_bit_cast(h2, (x & 0x00f000f0u) | 0x64006400u);
-            const h2 v = j & 1 ? __builtin_elementwise_fma(high, h2{(f16_t)0.0625f, (f16_t)0.0625f}, h2{(f16_t)-64.f, (f16_t)-64.f})
-                               : low + h2{(f16_t)-1024.f, (f16_t)-1024.f};
+            const h2 v = j & 1 ? __builtin_elementwise_fma(__builtin_bit_cast(h2, and_or(x, HIGH, b.h1024)), h2{(f16_t)0.0625f, (f16_t)0.0625f},
+                                                           h2{(f16_t)-64.f, (f16_t)-64.f})
+                               : __builtin_bit_cast(h2, and_or(x, LOW, b.h1024)) + h2{(f16_t)-1024.f, (f16_t)-1024.f};
             r[j] = __builtin_bit_cast(uint32_t, v);
         }
         return r;
     }
 };
 
-// the four lanes of a column, a quarter of the wavefront apart
-__device__ __forceinline__ float quarters_max(float x)
+// over the four lanes of a column, a quarter of the wavefront apart: the swaps put the other half, then the other quarter, beside each lane's own
+template <class F>
+__device__ __forceinline__ float quarters(float x, F f)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    uint32_t u = __float_as_uint(x);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    u = __float_as_uint(f(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float quarters_sum(float x)
+__device__ __forceinline__ float quarters_max(float x) { return quarters(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float quarters_sum(float x) { return quarters(x, [](float a, float b) { return a + b; }); }
+
+// lane E of every quarter, to the whole quarter (as an operand of the instruction that uses it)
+template <int E>
+__device__ __forceinline__ float from_lane(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x150 + E, 0xf, 0xf, true));
+}
+template <int E = 0, class F>
+__device__ __forceinline__ void for8(F f)
+{
+    if constexpr (E < 8) {
+        f(std::integral_constant<int, E>());
+        for8<E + 1>(f);
+    }
 }
 
-// 32 tokens' codes and grids of one head, as a lane uses them
+// The pages of 32 tokens: of the first and the last 16 of them, as pages have 16 tokens at least.
+struct Pages { int first, last; };
+__device__ __forceinline__ Pages pages_of(const Kv4View& c, const int32_t* __restrict__ table, int max_pages, int t0)
+{
+    const int first = kv4_page(table, max_pages, c.pages, c.shift, t0);
+    return Pages{first, c.shift > 4 ? first : kv4_page(table, max_pages, c.pages, c.shift, t0 + 16)};
+}
+
+// 32 tokens of one head: where their rows are, and the grids of token 8 g + lane % 8.
+struct Where {
+    int64_t row0, row1;        // the cache rows of token 0, and (pages of 16) of token 16, less 16
+    bool first, last;          // whether the first and the last 16 tokens lie on a page
+};
+__device__ __forceinline__ Where where(const Kv4View& c, Pages p, int h, int t0)
+{
+    // tokens on no page: page 0 is read in their place, and masked
+    const int mask = (1 << c.shift) - 1;
+    Where w;
+    w.first = p.first >= 0;
+    w.last = p.last >= 0;
+    w.row0 = ((((int64_t)(w.first ? p.first : 0)) * c.heads + h) << c.shift) + (t0 & mask);
+    w.row1 = c.shift > 4 ? w.row0 : ((((int64_t)(w.last ? p.last : 0)) * c.heads + h) << c.shift) + ((t0 + 16) & mask) - 16;
+    return w;
+}
+// f(row of token 0), for a lane whose tokens are among the first or the last 16.  With pages of 32 tokens or more the row is a scalar.
+template <class F>
+__device__ __forceinline__ void at_token(const Kv4View& c, const Where& w, bool second, F f)
+{
+    const int64_t row0 = w.row0, row1 = w.row1;
+    if (c.shift > 4) f(row0);
+    else f(second ? row1 : row0);
+}
+
 template <int D> struct Tokens {
     static constexpr int K = D / 32, V = D / 128 > 0 ? D / 128 : 1;   // words of a K row, words of a V row (dim 64: half a word)
     uint32_t k[2][K];
     uint32_t v[8][V];
-    u4 kg[2], vg[2];
-    bool ok0, ok1;             // whether the first and the last 16 tokens lie on a page
+    uint32_t kg, vg;
+    bool first, last;
 };
 
+__device__ __forceinline__ void load_grids(const Kv4View& c, const Where& w, uint32_t& kg, uint32_t& vg)
+{
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const unsigned at = 8 * g + (lane & 7);
+    at_token(c, w, g & 2, [&](int64_t row) {
+        kg = (c.k_grids + row)[at];
+        vg = (c.v_grids + row)[at];
+    });
+}
+
 template <int D>
-__device__ __forceinline__ void load_tokens(const Kv4View& c, const int32_t* __restrict__ table, int max_pages, int h, int t0, Tokens<D>& x)
+__device__ __forceinline__ void load_tokens(const Kv4View& c, Pages p, int h, int t0, Tokens<D>& x)
 {
     constexpr int ROW = D / 2;
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-    const int p0 = kv4_page(table, max_pages, c.pages, c.shift, t0), p1 = kv4_page(table, max_pages, c.pages, c.shift, t0 + 16);
-    x.ok0 = p0 >= 0;
-    x.ok1 = p1 >= 0;
-    // tokens on no page: page 0 is read in their place, and masked
-    const int mask = (1 << c.shift) - 1;
-    const int64_t row0 = ((((int64_t)(p0 < 0 ? 0 : p0)) * c.heads + h) << c.shift) + (t0 & mask);
-    const int64_t row1 = ((((int64_t)(p1 < 0 ? 0 : p1)) * c.heads + h) << c.shift) + ((t0 + 16) & mask) - 16;
-    // K: row r of instruction i is token 8 (r / 4) + 4 i + r % 4
-    const int64_t kr = ((r & 8) ? row1 : row0) + 8 * (r >> 2) + (r & 3);
+    const Where w = where(c, p, h, t0);
+    x.first = w.first;
+    x.last = w.last;
+    // K: row r of instruction i is token 8 (r / 4) + 4 i + r % 4; V: row e of quarter g is token 8 g + e
+    at_token(c, w, r & 8, [&](int64_t row) {
+        const uint8_t* __restrict__ k = c.k_codes + row * ROW;
+        const unsigned off = (8 * (r >> 2) + (r & 3)) * ROW + 4 * Tokens<D>::K * g;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) __builtin_memcpy(x.k[i], __builtin_assume_aligned(c.k_codes + (kr + 4 * i) * ROW + 4 * Tokens<D>::K * g, D == 64 ? 8 : 16), sizeof x.k[i]);
-    const int64_t vr = ((g & 2) ? row1 : row0) + 8 * g;
-    const uint8_t* __restrict__ v = c.v_codes + vr * ROW + (D / 32) * r;
+        for (int i = 0; i < 2; ++i) __builtin_memcpy(x.k[i], __builtin_assume_aligned(k + off + 4 * i * ROW, D == 64 ? 8 : 16), sizeof x.k[i]);
+    });
+    at_token(c, w, g & 2, [&](int64_t row) {
+        const uint8_t* __restrict__ v = c.v_codes + row * ROW;
+        const unsigned off = 8 * g * ROW + (D / 32) * r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if constexpr (D == 64) x.v[e][0] = *reinterpret_cast<const uint16_t*>(v + e * ROW);
-        else __builtin_memcpy(x.v[e], __builtin_assume_aligned(v + e * ROW, 4 * Tokens<D>::V), sizeof x.v[e]);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        x.kg[i] = *reinterpret_cast<const u4*>(c.k_grids + vr + 4 * i);
-        x.vg[i] = *reinterpret_cast<const u4*>(c.v_grids + vr + 4 * i);
-    }
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (D == 64) x.v[e][0] = *reinterpret_cast<const uint16_t*>(v + off + e * ROW);
+            else __builtin_memcpy(x.v[e], __builtin_assume_aligned(v + off + e * ROW, 4 * Tokens<D>::V), sizeof x.v[e]);
+        }
+    });
+    load_grids(c, w, x.kg, x.vg);
 }
 
-// WAVES wavefronts; each has QT x 16 query rows: its own ones, or (SHARE) the workgroup's, of whose tokens it takes every WAVES-th tile.
+// What is taken off the values' codes, as fp16 with their offset: 1024 + zero for codes in the low half of a byte, 64 + zero (of
+// (1024 + 16 code) / 16) in the high half; of tokens 2 j and 2 j + 1 of the lane's eight.
+struct Zeros { h2 low[4], high[4]; };
+__device__ __forceinline__ Zeros value_zeros(uint32_t vg, const Bits& b)
+{
+    Zeros z;
+    for8([&](auto e) {
+        constexpr int E = decltype(e)::value;
+        if constexpr (E % 2 == 0) {
+            const uint32_t z0 = __builtin_amdgcn_mov_dpp(vg, 0x150 + E, 0xf, 0xf, true), z1 = __builtin_amdgcn_mov_dpp(vg, 0x151 + E, 0xf, 0xf, true);
+            const uint32_t both = __builtin_amdgcn_perm(z1, z0, 0x05040100u);
+            z.low[E / 2] = __builtin_bit_cast(h2, and_or(both, LOW, b.h1024));
+            z.high[E / 2] = __builtin_bit_cast(h2, and_or(both << 4, HIGH, b.h64));
+        }
+    });
+    return z;
+}
+// code - zero of channel n (of four) of the lane's eight tokens; pair[j]: the four channels' codes of tokens 2 j and 2 j + 1
+__device__ __forceinline__ u4 value_fragment(const uint32_t (&pair)[4], int n, const Zeros& z, const Bits& b)
+{
+    u4 vf;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t w = n < 2 ? pair[j] : pair[j] >> 8;
+        const h2 v = n & 1 ? __builtin_elementwise_fma(__builtin_bit_cast(h2, and_or(w, HIGH, b.h1024)), h2{(f16_t)0.0625f, (f16_t)0.0625f}, -z.high[j])
+                           : __builtin_bit_cast(h2, and_or(w, LOW, b.h1024)) - z.low[j];
+        vf[j] = __builtin_bit_cast(uint32_t, v);
+    }
+    return vf;
+}
+
+// WAVES wavefronts, each with QT x 16 query rows.
+//   SHARE: the same rows for all of them; each takes every WAVES-th tile of tokens into its registers, and their sums meet in LDS at the
+//     end.  For few rows, where the tokens are what costs.
+//   otherwise: rows of its own.  All need the same tokens: each turns a quarter of a tile's codes into fragments in LDS, a tile ahead, and
+//     reads all of them: the codes of 32 tokens take 140 vector instructions, a wavefront's softmax of 16 rows over them 80.
 template <class T, int D, int QT, bool SHARE>
-__global__ __launch_bounds__(256, SHARE ? 2 : 2) void kv4_attention_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
 {
     constexpr int WAVES = 4, M = D / 16, TILE = 16 * QT * (SHARE ? 1 : WAVES);
-    using X = Tokens<D>;
-    __shared__ float sh_o[SHARE ? WAVES : 1][SHARE ? 16 * QT * (D + 4) : 1];
+    __shared__ __attribute__((aligned(16))) float sh_o[SHARE ? WAVES : 1][SHARE ? 16 * QT * (D + 4) : 4];
     __shared__ float sh_ml[SHARE ? WAVES : 1][SHARE ? 16 * QT * 2 : 1];
+    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : 2 * M][SHARE ? 1 : 64];   // fragments of K, then of V
 
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = a.q.group;
+    const Bits bits = offset_bits();
 
     // the sequence and the rows of this workgroup: sequence b's tiles begin at floor(first row * G / TILE) + b, which leaves room for
     // every sequence's last, partial tile
     auto first_tile = [&](int b) { return (int64_t)kv4_rows(a.s.starts, b, a.s.rows).first * G / TILE + b; };
-    const int b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, (int64_t)blockIdx.x, first_tile));
+    // (few rows: in their order; many: the last ones first, which see most)
+    const int h = blockIdx.x % a.c.heads, place = blockIdx.x / a.c.heads, index = SHARE ? place : (int)(gridDim.x / a.c.heads) - 1 - place;
+    const int b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, index, first_tile));
     const Kv4Rows mine = kv4_rows(a.s.starts, b, a.s.rows);
     const int rows = mine.count * G;                                   // tokens x query heads of the kv head
-    const int64_t base64 = ((int64_t)blockIdx.x - first_tile(b)) * TILE;
+    const int64_t base64 = (index - first_tile(b)) * TILE;
     if (base64 < 0 || base64 >= rows) return;
     const int base = (int)base64 + (SHARE ? 0 : wave * 16 * QT);
-    const int h = blockIdx.y, part = blockIdx.z;
+    const int part = blockIdx.y;
     const int length = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
     const int before = length - mine.count;                            // position of the sequence's first new token (< 0: it is not there)
     const int32_t* __restrict__ table = a.s.table + (int64_t)b * a.s.table_ld;
@@ -200,8 +306,14 @@ __global__ __launch_bounds__(256, SHARE ? 2 : 2) void kv4_attention_kernel(AttnA
     const int any_to = base < rows ? max(0, to1) : 0, all_to = to0;
     const int any_from = a.q.window > 0 ? max(0, to0 - a.q.window) : 0, all_from = a.q.window > 0 ? max(0, to1 - a.q.window) : 0;
 
-    // this part's tokens, in tiles of 32
-    const int tile0 = any_from / 32, tile1 = (any_to + 31) / 32;
+    // this part's tokens, in tiles of 32; without SHARE the workgroup's rows, and `needed` those tiles that the wavefront's see
+    int wg_from = any_from, wg_to = any_to;
+    if constexpr (!SHARE) {
+        const int first = (int)base64, final = min(first + TILE, rows) - 1;
+        wg_to = max(0, a.q.causal ? before + final / G + 1 : length);
+        wg_from = a.q.window > 0 ? max(0, (a.q.causal ? before + first / G + 1 : length) - a.q.window) : 0;
+    }
+    const int tile0 = wg_from / 32, tile1 = (wg_to + 31) / 32;
     const int per = max((max(0, tile1 - tile0) + a.parts - 1) / a.parts, KV4_PART / 32);
     const int begin = tile0 + part * per, end = min(tile1, begin + per);
 
@@ -215,109 +327,192 @@ __global__ __launch_bounds__(256, SHARE ? 2 : 2) void kv4_attention_kernel(AttnA
         for (int j = 0; j < M; ++j) o[t][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int step = SHARE ? WAVES : 1;
-    int tile = begin + (SHARE ? wave : 0);
-    X x;
-    if (tile < end) load_tokens<D>(a.c, table, a.s.max_pages, h, tile * 32, x);
-    for (; tile < end; tile += step) {
-        X next;
-        if (tile + step < end) load_tokens<D>(a.c, table, a.s.max_pages, h, (tile + step) * 32, next);
-        const int t0 = tile * 32;
-
-        // scores
+    // one tile of tokens: its scores, weights and share of the sums.  key(i, k), value(u, n): the fragments
+    auto attend = [&](int t0, uint32_t kg, uint32_t vg, bool first, bool final, auto key, auto value) {
+        // a lane works on the grids of one token; the eight it needs come from the lanes of its quarter
+        const float ka = __uint_as_float(kg & 0xffff0000u) * a.scale2, kz = -(Frag<T>::OFFSET + (float)kv4_zero(kg));
+        const float va = __uint_as_float(vg & 0xffff0000u), vlog = (float)(max((int)(vg >> 23), 127 + VALUE_FLOOR) - 127);
+        float kas[8], vtop = vlog;
+        for8([&](auto e) {
+            constexpr int E = decltype(e)::value;
+            kas[E] = from_lane<E>(ka);
+            vtop = fmaxf(vtop, from_lane<E>(vlog));
+        });
         f4 s[QT][2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int t = 0; t < QT; ++t)
+            for8([&](auto e) { s[t][decltype(e)::value >> 2][decltype(e)::value & 3] = from_lane<decltype(e)::value>(kz) * qsum[t]; });
 #pragma unroll
-            for (int t = 0; t < QT; ++t) s[t][i] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) {
-                const u4 kf = Frag<T>::codes(x.k[i][k]);
+                const u4 kf = key(i, k);
 #pragma unroll
                 for (int t = 0; t < QT; ++t) s[t][i] = Frag<T>::mfma(kf, qf[t][k], s[t][i]);
             }
-        }
-        const bool edge = !(x.ok0 && x.ok1 && t0 >= all_from && t0 + 32 <= all_to);
-        float ka[8], kz[8], va[8], vlog[8];
+        // u: scores above the running maximum, in binary orders
+        float u[QT][8], most = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t w = x.kg[e >> 2][e & 3], v = x.vg[e >> 2][e & 3];
-            ka[e] = __uint_as_float(w & 0xffff0000u) * a.scale2;
-            kz[e] = -(Frag<T>::OFFSET + (float)kv4_zero(w));
-            va[e] = __uint_as_float(v & 0xffff0000u);
-            vlog[e] = (float)max((int)(v >> 23) - 127, VALUE_FLOOR);
-        }
-        u4 pf[QT];
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            float y[8];
+            for (int e = 0; e < 8; ++e) u[t][e] = fmaf(s[t][e >> 2][e & 3], kas[e], -m[t]);
+        const bool edge = !(first && final && t0 >= all_from && t0 + 32 <= all_to);
+        if (edge) {
+            const bool page = (g & 2) ? final : first;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = fmaf(kz[e], qsum[t], s[t][e >> 2][e & 3]) * ka[e];
-            if (edge) {
+            for (int t = 0; t < QT; ++t)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int tok = t0 + 8 * g + e;
-                    if (tok < from[t] || tok >= to[t] || !((g & 2) ? x.ok1 : x.ok0)) y[e] = -INFINITY;
+                    if (tok < from[t] || tok >= to[t] || !page) u[t][e] = -INFINITY;
                 }
-            }
-            float top = y[0] + vlog[0];
+        }
 #pragma unroll
-            for (int e = 1; e < 8; ++e) top = fmaxf(top, y[e] + vlog[e]);
-            top = quarters_max(top);
-            if (__any(top > m[t] + RAISE)) {
-                const float up = fmaxf(m[t], top), f = __builtin_amdgcn_exp2f(m[t] - up);
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, u[t][e]);
+        // no weight can pass 2^RAISE; where one might, the maximum is raised to what the tokens have
+        if (__any(most + vtop > RAISE)) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                float z = -INFINITY;
+                for8([&](auto e) {
+                    constexpr int E = decltype(e)::value;
+                    if (u[t][E] != -INFINITY) {
+                        u[t][E] = s[t][E >> 2][E & 3] * kas[E];
+                        z = fmaxf(z, u[t][E] + from_lane<E>(vlog));
+                    }
+                });
+                const float up = fmaxf(m[t], quarters_max(z)), f = __builtin_amdgcn_exp2f(m[t] - up);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[t][e] -= up;
                 m[t] = up;
                 l[t] *= f;
 #pragma unroll
                 for (int j = 0; j < M; ++j) o[t][j] *= f;
             }
-            f16x8 p;
-            float sum = 0.f;
+        }
+        f16x8 p[QT];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(y[e] - m[t]);
-                sum += w;
-                p[e] = (f16_t)(w * va[e]);
-            }
-            if (edge) {
-                // also where the token's values are NaN
+        for (int t = 0; t < QT; ++t) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(u[t][e]);
+            l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            for8([&](auto e) { p[t][decltype(e)::value] = (f16_t)(w[decltype(e)::value] * from_lane<decltype(e)::value>(va)); });
+        }
+        if (edge) {
+            // nothing also where the token's values are NaN
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (y[e] == -INFINITY) p[e] = (f16_t)0.f;
+                    if (u[t][e] == -INFINITY) p[t][e] = (f16_t)0.f;
+        }
+#pragma unroll
+        for (int n = 0; n < M; ++n) {
+            const u4 vf = value(n >> 2, n & 3);
+#pragma unroll
+            for (int t = 0; t < QT; ++t) o[t][n] = Frag<f16_t>::mfma(vf, __builtin_bit_cast(u4, p[t]), o[t][n]);
+        }
+    };
+    auto pages = [&](int i) { return pages_of(a.c, table, a.s.max_pages, (i < end ? i : begin) * 32); };
+    if constexpr (SHARE) {
+        // the pages two tiles ahead and the tokens of the next tile are on their way while a tile is attended to
+        int tile = begin + wave;
+        if (tile < end) {
+            using X = Tokens<D>;
+            X x0, x1;
+            auto use = [&](X& x) {
+                const Zeros z = value_zeros(x.vg, bits);
+                uint32_t pair[4];
+                attend(tile * 32, x.kg, x.vg, x.first, x.last, [&](int i, int k) { return Frag<T>::codes(x.k[i][k], bits); },
+                       [&](int u, int n) {
+                           if (n == 0)
+#pragma unroll
+                               for (int j = 0; j < 4; ++j)
+                                   pair[j] = __builtin_amdgcn_perm(x.v[2 * j + 1][u / 2], x.v[2 * j][u / 2], u & 1 ? 0x07060302u : 0x05040100u);
+                           return value_fragment(pair, n, z, bits);
+                       });
+            };
+            load_tokens<D>(a.c, pages(tile), h, tile * 32, x0);
+            Pages next = pages(tile + WAVES);
+            for (;;) {
+                if (tile + WAVES < end) load_tokens<D>(a.c, next, h, (tile + WAVES) * 32, x1);
+                next = pages(tile + 2 * WAVES);
+                use(x0);
+                if ((tile += WAVES) >= end) break;
+                if (tile + WAVES < end) load_tokens<D>(a.c, next, h, (tile + WAVES) * 32, x0);
+                next = pages(tile + 2 * WAVES);
+                use(x1);
+                if ((tile += WAVES) >= end) break;
             }
-            l[t] += sum;
-            pf[t] = __builtin_bit_cast(u4, p);
         }
-        // values: 8 tokens x (D / 16) codes of this lane, four channels (16 bits) at a time
-        h2 off_low[4], off_high[4];
+    } else if (begin < end) {
+        // this wavefront's share of a tile: D / 64 fragments of K (numbers i D / 32 + k) and as many of V (4 u + n)
+        constexpr int SHARE_OF = D / 64, ROW = D / 2;
+        struct Raw { uint32_t k[SHARE_OF], v[8], kg, vg; bool first, last; };
+        auto load = [&](Pages p, int t0, Raw& x) {
+            const Where w = where(a.c, p, h, t0);
+            const int r = col;
+            x.first = w.first;
+            x.last = w.last;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t z = kv4_zero(x.vg[j >> 1][2 * (j & 1)]) | kv4_zero(x.vg[j >> 1][2 * (j & 1) + 1]) << 16;
-            off_low[j] = __builtin_bit_cast(h2, z | 0x64006400u);              // 1024 + zero
-            off_high[j] = __builtin_bit_cast(h2, z << 4 | 0x54005400u);        // 64 + zero
-        }
+            for (int j = 0; j < SHARE_OF; ++j) {
+                const int f = wave * SHARE_OF + j, i = f / (D / 32), k = f % (D / 32);
+                at_token(a.c, w, r & 8, [&](int64_t row) {
+                    x.k[j] = *reinterpret_cast<const uint32_t*>(a.c.k_codes + row * ROW + ((8 * (r >> 2) + (r & 3) + 4 * i) * ROW + (D / 8) * g + 4 * k));
+                });
+            }
+            const int f = wave * SHARE_OF, u = f >> 2;                 // (all of a wavefront's fragments of V are of the same four channels)
+            at_token(a.c, w, g & 2, [&](int64_t row) {
 #pragma unroll
-        for (int u = 0; u < D / 64; ++u) {
+                for (int e = 0; e < 8; ++e)
+                    x.v[e] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + ((8 * g + e) * ROW + (D / 32) * r + 2 * u));
+            });
+            load_grids(a.c, w, x.kg, x.vg);
+        };
+        auto stage = [&](int buf, const Raw& x) {
+#pragma unroll
+            for (int j = 0; j < SHARE_OF; ++j) sh_f[buf][wave * SHARE_OF + j][lane] = Frag<T>::codes(x.k[j], bits);
+            const Zeros z = value_zeros(x.vg, bits);
             uint32_t pair[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                pair[j] = __builtin_amdgcn_perm(x.v[2 * j + 1][u / 2], x.v[2 * j][u / 2], u & 1 ? 0x07060302u : 0x05040100u);
+            for (int j = 0; j < 4; ++j) pair[j] = x.v[2 * j] | x.v[2 * j + 1] << 16;
+            const int n0 = (wave * SHARE_OF) & 3;
+            if constexpr (SHARE_OF == 4) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                u4 vf;
+                for (int n = 0; n < 4; ++n) sh_f[buf][M + wave * 4 + n][lane] = value_fragment(pair, n, z, bits);
+            } else {
+                // the first channel is 0 or 2 (dim 128), or the wavefront's number (dim 64): the same for all lanes
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t w = n < 2 ? pair[j] : pair[j] >> 8;
-                    const h2 v = n & 1 ? __builtin_elementwise_fma(__builtin_bit_cast(h2, (w & 0x00f000f0u) | 0x64006400u),
-                                                                  h2{(f16_t)0.0625f, (f16_t)0.0625f}, -off_high[j])
-                                       : __builtin_bit_cast(h2, (w & 0x000f000fu) | 0x64006400u) - off_low[j];
-                    vf[j] = __builtin_bit_cast(uint32_t, v);
-                }
-#pragma unroll
-                for (int t = 0; t < QT; ++t) o[t][4 * u + n] = Frag<f16_t>::mfma(vf, pf[t], o[t][4 * u + n]);
+                for (int n = 0; n < 4; ++n)
+                    if (n >= n0 && n < n0 + SHARE_OF) sh_f[buf][M + wave * SHARE_OF + n - n0][lane] = value_fragment(pair, n, z, bits);
             }
+        };
+        Raw x;
+        load(pages(begin), begin * 32, x);
+        Pages next = pages(begin + 1);
+        stage(0, x);
+        uint32_t kg = x.kg, vg = x.vg;
+        bool first = x.first, final = x.last;
+        if (begin + 1 < end) load(next, (begin + 1) * 32, x);
+        next = pages(begin + 2);
+        for (int tile = begin; tile < end; ++tile) {
+            const int buf = (tile - begin) & 1;
+            // this tile's fragments are in LDS, and everybody is done with the other buffer
+            __syncthreads();
+            const uint32_t kg1 = x.kg, vg1 = x.vg;
+            const bool first1 = x.first, final1 = x.last;
+            if (tile + 1 < end) stage(buf ^ 1, x);
+            if (tile + 2 < end) load(next, (tile + 2) * 32, x);
+            next = pages(tile + 3);
+            const int t0 = tile * 32;
+            if (t0 < any_to && t0 + 32 > any_from)
+                attend(t0, kg, vg, first, final, [&](int i, int k) { return sh_f[buf][i * (D / 32) + k][lane]; },
+                       [&](int u, int n) { return sh_f[buf][M + 4 * u + n][lane]; });
+            kg = kg1; vg = vg1; first = first1; final = final1;
         }
-        x = next;
     }
 
     // sums over the four lanes of a column
@@ -440,7 +635,7 @@ Kv4Plan kv4_attention_plan(int cus, int dim, int heads, int group, int n_seqs, i
     p.tiles = rows * group / p.tile + n_seqs;
     const int64_t have = std::max<int64_t>(1, p.tiles * heads);
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(KV4_MAX_PARTS, (longest + KV4_PART - 1) / KV4_PART));
-    p.parts = (int)std::min<int64_t>(most, std::max<int64_t>(1, (4 * (int64_t)cus + have - 1) / have));
+    p.parts = (int)std::min<int64_t>(most, std::max<int64_t>(1, ((p.share ? 8 : 2) * (int64_t)cus + have - 1) / have));
     return p;
 }
 
@@ -452,7 +647,7 @@ int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads, int group,
 template <class T, int D>
 static hipError_t attention_of(hipStream_t st, const Kv4Plan& p, const AttnArgs& a)
 {
-    const dim3 grid((unsigned)p.tiles, (unsigned)a.c.heads, (unsigned)p.parts), block(256);
+    const dim3 grid((unsigned)(p.tiles * a.c.heads), (unsigned)p.parts), block(256);
     if (p.share && p.tile == 16) hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, true>), grid, block, 0, st, a);
     else if constexpr (D == 256) hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, false>), grid, block, 0, st, a);
     else if (p.share) hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, true>), grid, block, 0, st, a);
