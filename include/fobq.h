@@ -283,7 +283,7 @@ int fobq_fp8_from_codes(fobq_ctx* ctx, const uint8_t* codes, const float* scales
                         const fobq_fp8_matrix* out);
 
 /* Y = A B^T: Y[m][n] = sum over columns of A's element (m, c) times B's element (n, c).  A: the activations, rows_per_scale 1;
- * B: the weights, rows_per_scale 1 or 128, as many columns; the formats may differ.  Y: device, `type`, A->rows x B->rows, row
+ * B: the weights, rows_per_scale 1 or 128, as many columns; the formats may differ; both ld below 2^24.  Y: device, `type`, A->rows x B->rows, row
  * stride ld >= B->rows elements.  Sums in fp32, rounded to `type` once; the same bits in every run on equal arguments.
  * work: at least fobq_fp8_matmul_workspace's bytes (0: may be NULL), 16-byte aligned. */
 int fobq_fp8_matmul(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8_matrix* B, void* Y, int32_t type, int64_t ld,
@@ -443,7 +443,7 @@ int fobq_debug_offset_tables(int32_t k, int32_t pad, int64_t h, int64_t w, int32
  *                  out: tile edge, slabs of an accumulation, slabs that this call can touch
  *   FOBQ_PLAN_SLABS  in: channels, kernel size of a stride-1 convolution, integer slices
  *                  out: slabs that fobq_hessian_begin reserves, slabs that its form by tap offsets takes (0: another form)
- *   FOBQ_PLAN_FP8_MATMUL  in: compute units, m, n, k, type of the result (fobq_float)
+ *   FOBQ_PLAN_FP8_MATMUL  in: compute units, m, n, k, type of the result (fobq_float), rows of B to a scale
  *                  out: rows of A and of B of a tile, parts of the contraction, blocks of 128 a part, bytes of work
  *   FOBQ_PLAN_KV4_ATTENTION  in: compute units, head_dim, heads, group, n_seqs, rows, longest sequence
  *                  out: query rows of a workgroup, whether its wavefronts share them, parts of the tokens, workgroups a head and part, bytes of work

@@ -5,6 +5,8 @@ namespace fobq {
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 29;      // rows and columns of a matrix, packed rows: products with 4 stay in 32 bits
 
+constexpr int64_t MAX_APART = (int64_t)1 << 24;     // rows of a product's matrices: 256 of them stay within 32-bit offsets
+
 static int enter(fobq_ctx* ctx, const DeviceGuard& g) { return g.ok ? FOBQ_OK : set_err(ctx, FOBQ_EHIP, "cannot select device %d", ctx->device); }
 
 static bool aligned(const void* p, int to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -79,11 +81,11 @@ static int check_attention(fobq_ctx* ctx, const fobq_kv4_cache* c, const fobq_kv
 
 int lowbit_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* out, int32_t n_out)
 {
-    if (what == FOBQ_PLAN_FP8_MATMUL && n_in == 5 && n_out == 5) {
+    if (what == FOBQ_PLAN_FP8_MATMUL && n_in == 6 && n_out == 5) {
         for (int i = 0; i < 4; ++i)
             if (in[i] < (i ? 0 : 16) || in[i] >= (i ? MAX_SIDE : 4096)) return FOBQ_EINVAL;
-        if (!is_float((int)in[4])) return FOBQ_EINVAL;
-        const Fp8Plan p = fp8_matmul_plan((int)in[0], in[1], in[2], in[3], (int)in[4]);
+        if (!is_float((int)in[4]) || (in[5] != 1 && in[5] != 128)) return FOBQ_EINVAL;
+        const Fp8Plan p = fp8_matmul_plan((int)in[0], in[1], in[2], in[3], (int)in[4], (int)in[5]);
         out[0] = p.tm; out[1] = p.tn; out[2] = p.parts; out[3] = p.blocks_per_part; out[4] = fp8_matmul_workspace(p, in[1], in[2]);
         return FOBQ_OK;
     }
@@ -178,7 +180,7 @@ int fobq_fp8_matmul_workspace(fobq_ctx* ctx, int64_t m, int64_t n, int64_t k, in
     if (!bytes || m < 0 || n < 0 || k < 0 || m >= MAX_SIDE || n >= MAX_SIDE || k >= MAX_SIDE)
         return set_err(ctx, FOBQ_EINVAL, "bytes is NULL, or a size is not in 0..%lld", (long long)MAX_SIDE - 1);
     if (!is_float(type)) return set_err(ctx, FOBQ_EINVAL, "unknown type %d", type);
-    *bytes = fp8_matmul_workspace(fp8_matmul_plan(ctx->cus, m, n, k, type), m, n);
+    *bytes = fp8_matmul_workspace(fp8_matmul_plan(ctx->cus, m, n, k, type, 128), m, n);
     return FOBQ_OK;
 }
 
@@ -191,11 +193,13 @@ int fobq_fp8_matmul(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8_matr
     if (rc) return rc;
     if (a.per != 1) return set_err(ctx, FOBQ_EINVAL, "A must have a scale per row");
     if (a.cols != b.cols) return set_err(ctx, FOBQ_EINVAL, "A has %d columns, B %d", a.cols, b.cols);
+    if (a.ld >= MAX_APART || b.ld >= MAX_APART)
+        return set_err(ctx, FOBQ_EINVAL, "rows must be less than %lld bytes apart", (long long)MAX_APART);
     if (!is_float(type)) return set_err(ctx, FOBQ_EINVAL, "unknown type %d", type);
     if (ld < b.rows) return set_err(ctx, FOBQ_EINVAL, "ld (%lld) is less than the rows of B", (long long)ld);
     if (a.rows == 0 || b.rows == 0) return FOBQ_OK;
     if (!Y || !aligned(Y, float_size(type))) return set_err(ctx, FOBQ_EINVAL, "Y is NULL or not aligned to its elements");
-    const Fp8Plan p = fp8_matmul_plan(ctx->cus, a.rows, b.rows, a.cols, type);
+    const Fp8Plan p = fp8_matmul_plan(ctx->cus, a.rows, b.rows, a.cols, type, b.per);
     const int64_t need = fp8_matmul_workspace(p, a.rows, b.rows);
     if (work_bytes < need || (need > 0 && (!work || !aligned(work, 16))))
         return set_err(ctx, FOBQ_EINVAL, "work must be %lld bytes, 16-byte aligned (got %lld)", (long long)need, (long long)work_bytes);

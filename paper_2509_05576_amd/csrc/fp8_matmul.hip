@@ -11,9 +11,9 @@
 // The instruction's rows are rows of B (outputs n), its columns rows of A (inputs m): a lane's four results are four consecutive n of
 // one m, so sa is one value per lane and with a scale per 128 rows of B sb is the same for the whole wavefront.
 //
-// Tiles of both matrices are copied straight into LDS, 128 bytes a row, the 16-byte pieces of row r at places p ^ (r / 2 % 8): the 16
-// rows that the lanes of a quarter read at once then lie in all 64 banks.  Which eight k's a lane holds does not matter, as both
-// operands have the same.
+// Tiles of both matrices are copied straight into LDS, 128 bytes a row, the 16-byte pieces of row r at places p ^ ((r ^ r / 8 % 2) % 8):
+// eight rows, and 16, that lanes read at once then lie in all banks (with r / 2 % 8 a read took four cycles more).  Which k's a lane holds does
+// not matter, as both operands have the same.
 #include "lowbit.h"
 
 #include <algorithm>
@@ -74,12 +74,19 @@ __device__ __forceinline__ auto operand(i8v x)
     else return x;
 }
 
-__device__ __forceinline__ void copy16(const void* src, void* lds_base)
+// 16 bytes a lane from `offset` of a run of memory into LDS, lane after lane.  Behind the run's end nothing is read.
+typedef __amdgpu_buffer_rsrc_t Run;
+__device__ __forceinline__ Run run_of(const uint8_t* p, int64_t bytes)
 {
-    __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)src, (void __attribute__((address_space(3)))*)lds_base, 16, 0, 0);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(uint32_t)min(bytes, (int64_t)0xffffffff), 0x00020000);
+}
+__device__ __forceinline__ void copy16(Run run, unsigned offset, void* lds_base)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(run, (void __attribute__((address_space(3)))*)lds_base, 16, (int)offset, 0, 0, 0);
 }
 
-__device__ __forceinline__ int swizzle(int row, int piece) { return piece ^ (row >> 1 & 7); }
+// the place of a row's 16-byte piece
+__device__ __forceinline__ int swizzle(int row, int piece) { return piece ^ ((row ^ (row >> 3 & 1)) & 7); }
 
 // four consecutive n of row m
 __device__ __forceinline__ void put4(const MatmulArgs& g, int part, int m, int n, f4 v)
@@ -113,6 +120,8 @@ __device__ __forceinline__ void put4(const MatmulArgs& g, int part, int m, int n
     else out((f16_t)0.f);
 }
 
+constexpr int FEW_WAVES = 8;      // wavefronts of a workgroup for few rows
+
 // TM x TN outputs by WM x WN wavefronts.  FA, FB: the types of A and B; PER: rows of B to a scale.
 template <int TM, int TN, int WM, int WN, int FA, int FB, int PER, bool EXACT>
 __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
@@ -123,42 +132,49 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
     const int q = lane >> 4, c = lane & 15;
     const int wm = wave / WN, wn = wave % WN;
     const int M = g.a.rows, N = g.b.rows, K = g.a.cols, blocks = (K + 127) / 128;
-    const int m0 = blockIdx.x * TM, n0 = blockIdx.y * TN, part = blockIdx.z;
+    // Workgroups go to the 8 XCDs in turn.  Each XCD has a run of tiles, in strips of 4 tile rows, so that the ones it works on at a
+    // time share rows of A and of B in its L2.
+    const int tiles_m = (M + TM - 1) / TM, tiles_n = (N + TN - 1) / TN, tiles = tiles_m * tiles_n;
+    const int xcd = blockIdx.x % 8, first = tiles / 8 * xcd + min(xcd, tiles % 8), at = first + (int)blockIdx.x / 8;
+    const int strip = at / (4 * tiles_n), in_strip = at - strip * 4 * tiles_n, high = min(4, tiles_m - 4 * strip);
+    const int m0 = (4 * strip + in_strip % high) * TM, n0 = in_strip / high * TN, part = blockIdx.y;
     const int kb0 = part * g.per_part, kb1 = min(blocks, kb0 + g.per_part);
 
-    // pieces of a step's tiles, 16 bytes a thread: rows of A, then rows of B; rows behind the last are the last again
-    constexpr int PIECES = (TM + TN) * 8 / THREADS;
-    static_assert((TM * 8) % THREADS == 0 && (TN * 8) % THREADS == 0, "whole wavefronts of pieces");
-    auto source = [&](int i, int kb) -> const uint8_t* {
-        const int piece = i * THREADS + threadIdx.x, row = piece >> 3, k = swizzle(row, piece & 7) * 16;
-        return row < TM ? g.a.values + (int64_t)min(m0 + row, M - 1) * g.a.ld + (int64_t)kb * 128 + k
-                        : g.b.values + (int64_t)min(n0 + row - TM, N - 1) * g.b.ld + (int64_t)kb * 128 + k;
-    };
+    // A tile is copied 16 bytes a thread and piece, its rows in LDS one after another: a piece is THREADS / 8 rows below the one before.
+    // Rows behind the last read as zeros.
+    constexpr int PA = TM * 8 / THREADS, PB = TN * 8 / THREADS, STEP = THREADS / 8;
+    static_assert(TM % STEP == 0 && TN % STEP == 0 && STEP % 16 == 0, "pieces of whole rows, the same place in each");
+    const int row = threadIdx.x >> 3, column = swizzle(row, threadIdx.x & 7) * 16;
+    const Run ra = run_of(g.a.values + m0 * g.a.ld, (M - m0) * g.a.ld), rb = run_of(g.b.values + n0 * g.b.ld, (N - n0) * g.b.ld);
+    const unsigned lda = (unsigned)g.a.ld, ldb = (unsigned)g.b.ld, oa = row * lda + column, ob = row * ldb + column;
     auto fetch = [&](int buf, int kb) {
-        if (kb * 128 + 128 <= K) {
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) copy16(source(i, kb), &sh[buf][(i * THREADS + wave * 64) * 16]);
-        } else {
-            // the last block of columns is not whole: what is behind it counts as zero, whatever the rows hold there
+        for (int i = 0; i < PA; ++i) copy16(ra, oa + (i * STEP) * lda + (unsigned)kb * 128, &sh[buf][(i * THREADS + wave * 64) * 16]);
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const int piece = i * THREADS + threadIdx.x, row = piece >> 3, k = kb * 128 + swizzle(row, piece & 7) * 16;
-                uint32_t w[4] = {0, 0, 0, 0};
-                if (k < K) {
-                    __builtin_memcpy(w, __builtin_assume_aligned(source(i, kb), 16), 16);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int have = K - k - 4 * j;
-                        w[j] &= have >= 4 ? 0xffffffffu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
-                    }
-                }
-                __builtin_memcpy(__builtin_assume_aligned(&sh[buf][piece * 16], 16), w, 16);
-            }
-        }
+        for (int i = 0; i < PB; ++i) copy16(rb, ob + (i * STEP) * ldb + (unsigned)kb * 128, &sh[buf][TM * 128 + (i * THREADS + wave * 64) * 16]);
     };
-    auto fragment = [&](int buf, int row) {
-        const uint8_t* p = &sh[buf][row * 128];
-        const i4 lo = *reinterpret_cast<const i4*>(p + swizzle(row, 2 * q) * 16), hi = *reinterpret_cast<const i4*>(p + swizzle(row, 2 * q + 1) * 16);
+    // the last block of columns where it is not whole: what is behind it counts as zero, whatever the rows hold there
+    auto fetch_rest = [&](int buf, int kb) {
+        const int k = kb * 128 + column, left = K - k;
+        auto piece = [&](const Fp8View& x, int at, int rows, uint8_t* dst) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (left > 0 && at < rows) {
+                __builtin_memcpy(w, __builtin_assume_aligned(x.values + at * x.ld + k, 16), 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int have = left - 4 * j;
+                    w[j] &= have >= 4 ? 0xffffffffu : have <= 0 ? 0u : (1u << (8 * have)) - 1;
+                }
+            }
+            __builtin_memcpy(__builtin_assume_aligned(dst, 16), w, 16);
+        };
+        for (int i = 0; i < PA; ++i) piece(g.a, m0 + i * STEP + row, M, &sh[buf][(i * THREADS + threadIdx.x) * 16]);
+        for (int i = 0; i < PB; ++i) piece(g.b, n0 + i * STEP + row, N, &sh[buf][TM * 128 + (i * THREADS + threadIdx.x) * 16]);
+    };
+    const int p0 = swizzle(c, 2 * q) * 16, p1 = swizzle(c, 2 * q + 1) * 16;
+    auto fragment = [&](int buf, int first_row) {
+        const uint8_t* p = &sh[buf][(first_row + c) * 128];
+        const i4 lo = *reinterpret_cast<const i4*>(p + p0), hi = *reinterpret_cast<const i4*>(p + p1);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
@@ -169,40 +185,63 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
         for (int j = 0; j < SN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
     const int wm0 = wm * (TM / WM), wn0 = wn * (TN / WN);
-    if (kb0 < kb1) fetch(0, kb0);
-    for (int kb = kb0; kb < kb1; ++kb) {
-        const int buf = (kb - kb0) & 1;
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        if (kb + 1 < kb1) fetch(buf ^ 1, kb + 1);
-        float sa[SM];
-        f4 sb[PER == 1 ? SN : 1];
+    // the scales of a block: one of A for each of this lane's rows; of B (in PER == 1) four for each of its column groups
+    struct Scales { float a[SM]; f4 b[PER == 1 ? SN : 1]; };
+    auto scales = [&](int kb, Scales& s) {
 #pragma unroll
-        for (int i = 0; i < SM; ++i) sa[i] = g.a.scales[kb * g.a.ld_scales + min(m0 + wm0 + 16 * i + c, M - 1)];
+        for (int i = 0; i < SM; ++i) s.a[i] = g.a.scales[kb * g.a.ld_scales + min(m0 + wm0 + 16 * i + c, M - 1)];
         if constexpr (PER == 1) {
 #pragma unroll
             for (int j = 0; j < SN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sb[j][e] = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0 + 16 * j + 4 * q + e, N - 1)];
+                for (int e = 0; e < 4; ++e) s.b[j][e] = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0 + 16 * j + 4 * q + e, N - 1)];
         } else {
-            const float s = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0, N - 1) / 128];
-#pragma unroll
-            for (int i = 0; i < SM; ++i) sa[i] *= s;
+            s.b[0][0] = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0, N - 1) / 128];
         }
+    };
+    auto multiply = [&](int buf, const Scales& s) {
+        float sa[SM];
+#pragma unroll
+        for (int i = 0; i < SM; ++i) sa[i] = PER == 1 ? s.a[i] : s.a[i] * s.b[0][0];
         decltype(operand<EXACT, FB>(i8v())) bf[SN];
 #pragma unroll
-        for (int j = 0; j < SN; ++j) bf[j] = operand<EXACT, FB>(fragment(buf, TM + wn0 + 16 * j + c));
+        for (int j = 0; j < SN; ++j) bf[j] = operand<EXACT, FB>(fragment(buf, TM + wn0 + 16 * j));
 #pragma unroll
         for (int i = 0; i < SM; ++i) {
-            const auto af = operand<EXACT, FA>(fragment(buf, wm0 + 16 * i + c));
+            const auto af = operand<EXACT, FA>(fragment(buf, wm0 + 16 * i));
 #pragma unroll
             for (int j = 0; j < SN; ++j) {
                 f4 p = mfma_block<FB, FA>(bf[j], af);
-                if constexpr (PER == 1) p *= sb[j];
+                if constexpr (PER == 1) p *= s.b[j];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], sa[i], acc[i][j][e]);
             }
         }
+    };
+    const int whole = min(kb1, K / 128);                     // blocks of this part that are whole
+    Scales next;
+    if (kb0 < whole) {
+        scales(kb0, next);
+        fetch(0, kb0);
+    }
+    for (int kb = kb0; kb < whole; ++kb) {
+        const int buf = (kb - kb0) & 1;
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        const Scales s = next;
+        // (in this order: the scales would otherwise be waited for behind the copies, which are not needed until the next block)
+        if (kb + 1 < whole) {
+            scales(kb + 1, next);
+            fetch(buf ^ 1, kb + 1);
+        }
+        multiply(buf, s);
+    }
+    if (whole < kb1) {
+        __syncthreads();
+        fetch_rest(0, whole);
+        scales(whole, next);
+        __syncthreads();
+        multiply(0, next);
     }
 #pragma unroll
     for (int i = 0; i < SM; ++i) {
@@ -213,6 +252,93 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
                 const int n = n0 + wn0 + 16 * j + 4 * q;
                 if (n < N) put4(g, part, m, n, acc[i][j]);
             }
+    }
+}
+
+// Few rows of A: the weights are read once, straight into the registers of the wavefront that multiplies them, 128 bytes of 16 rows in
+// two loads.  A workgroup has 16 rows of B; its wavefronts deal the blocks among them, four at a time (8 KiB of weights in flight each), and
+// add up in LDS, in their order.  On fp16 values throughout: conversions are hidden behind memory.
+template <int MT, int FA, int FB, int PER>
+__global__ __launch_bounds__(64 * FEW_WAVES) void fp8_matmul_few_kernel(MatmulArgs g)
+{
+    constexpr int AT_ONCE = MT == 1 ? 4 : 2;
+    __shared__ f4 sum[FEW_WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+    const int M = g.a.rows, N = g.b.rows, K = g.a.cols, blocks = (K + 127) / 128;
+    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
+    const uint8_t* __restrict__ brow = g.b.values + (int64_t)min(n0 + c, N - 1) * g.b.ld + 32 * q;
+    const uint8_t* __restrict__ arow[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) arow[i] = g.a.values + (int64_t)min(m0 + 16 * i + c, M - 1) * g.a.ld + 32 * q;
+    f4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
+
+    auto load = [&](const uint8_t* __restrict__ row, int kb) {
+        i4 lo, hi;
+        const int k = kb * 128 + 32 * q;
+        if (kb * 128 + 128 <= K) {
+            lo = *reinterpret_cast<const i4*>(row + (int64_t)kb * 128);
+            hi = *reinterpret_cast<const i4*>(row + (int64_t)kb * 128 + 16);
+        } else {
+            // the last block, which is not whole, and those behind it: nothing is read there
+            auto piece = [&](int at) {
+                i4 w = {0, 0, 0, 0};
+                if (at < K) {
+                    w = *reinterpret_cast<const i4*>(row + (at - 32 * q));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int have = K - at - 4 * j;
+                        w[j] &= have >= 4 ? -1 : have <= 0 ? 0 : (1 << (8 * have)) - 1;
+                    }
+                }
+                return w;
+            };
+            lo = piece(k);
+            hi = piece(k + 16);
+        }
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    for (int kb0 = wave * AT_ONCE; kb0 < blocks; kb0 += FEW_WAVES * AT_ONCE) {
+        i8v b[AT_ONCE], a[AT_ONCE][MT];
+        float sa[AT_ONCE][MT], sb[AT_ONCE][PER == 1 ? 4 : 1];
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x) {
+            b[x] = load(brow, kb0 + x);
+            const int kb = min(kb0 + x, blocks - 1);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                a[x][i] = load(arow[i], kb0 + x);
+                sa[x][i] = g.a.scales[kb * g.a.ld_scales + min(m0 + 16 * i + c, M - 1)];
+            }
+            if constexpr (PER == 1) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sb[x][e] = g.b.scales[kb * g.b.ld_scales + min(n0 + 4 * q + e, N - 1)];
+            } else {
+                sb[x][0] = g.b.scales[kb * g.b.ld_scales + n0 / 128];
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x) {
+            if (kb0 + x >= blocks) break;
+            const auto bf = as_fp16<FB>(b[x]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const f4 p = mfma_block<FB, FA>(bf, as_fp16<FA>(a[x][i]));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(p[e] * sb[x][PER == 1 ? e : 0], sa[x][i], acc[i][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sum[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave < MT) {
+        f4 v = sum[0][wave][lane];
+#pragma unroll
+        for (int k = 1; k < FEW_WAVES; ++k) v += sum[k][wave][lane];
+        const int m = m0 + 16 * wave + c, n = n0 + 4 * q;
+        if (m < M && n < N) put4(g, 0, m, n, v);
     }
 }
 
@@ -241,10 +367,19 @@ __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(MatmulArgs g)
     put4(whole, 0, (int)m, n, sum);
 }
 
-Fp8Plan fp8_matmul_plan(int cus, int64_t m, int64_t n, int64_t k, int type)
+Fp8Plan fp8_matmul_plan(int cus, int64_t m, int64_t n, int64_t k, int type, int per)
 {
     Fp8Plan p;
-    p.tm = p.tn = 128;
+    if (m <= 32) {
+        p.tm = m <= 16 ? 16 : 32;
+        p.tn = 16;
+        p.parts = 1;
+        p.blocks_per_part = std::max<int64_t>(1, (k + 127) / 128);
+        return p;
+    }
+    // 256 x 256 tiles where they fill the chip; with results in 32 bits, or a scale per row of B, their operands do not fit the registers
+    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
+    p.tm = p.tn = type != FOBQ_F32 && per == 128 && large >= cus ? 256 : 128;
     const int64_t tiles = std::max<int64_t>(1, ((m + p.tm - 1) / p.tm) * ((n + p.tn - 1) / p.tn)), blocks = (k + 127) / 128;
     const int64_t want = std::min<int64_t>(std::max<int64_t>(1, cus / tiles), std::max<int64_t>(1, blocks / 4));
     p.blocks_per_part = std::max<int64_t>(1, (blocks + want - 1) / want);
@@ -257,9 +392,17 @@ int64_t fp8_matmul_workspace(const Fp8Plan& p, int64_t m, int64_t n) { return p.
 template <int FA, int FB, int PER>
 static hipError_t matmul_of(hipStream_t s, const Fp8Plan& p, const MatmulArgs& g)
 {
-    const dim3 grid((unsigned)((g.a.rows + p.tm - 1) / p.tm), (unsigned)((g.b.rows + p.tn - 1) / p.tn), (unsigned)p.parts);
+    const dim3 grid((unsigned)(((g.a.rows + p.tm - 1) / p.tm) * ((g.b.rows + p.tn - 1) / p.tn)), (unsigned)p.parts);
+    if (p.tn == 16) {
+        const dim3 few((unsigned)((g.b.rows + 15) / 16), (unsigned)((g.a.rows + p.tm - 1) / p.tm)), block(64 * FEW_WAVES);
+        if (p.tm == 16) hipLaunchKernelGGL((fp8_matmul_few_kernel<1, FA, FB, PER>), few, block, 0, s, g);
+        else hipLaunchKernelGGL((fp8_matmul_few_kernel<2, FA, FB, PER>), few, block, 0, s, g);
+        return hipGetLastError();
+    }
     if (g.type == FOBQ_F32) hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
-    else hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+    else if (p.tm == 256) {
+        if constexpr (PER == 128) hipLaunchKernelGGL((fp8_matmul_kernel<256, 256, 2, 4, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
+    } else hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     const int64_t items = (int64_t)g.a.rows * ((g.b.rows + 3) / 4);

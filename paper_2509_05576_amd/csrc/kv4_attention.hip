@@ -29,6 +29,7 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 
 constexpr float NEG_MAX = -3.402823466e38f;
 constexpr int VALUE_FLOOR = -88;
@@ -126,11 +127,26 @@ __device__ __forceinline__ void for8(F f)
 
 // The pages of 32 tokens: of the first and the last 16 of them, as pages have 16 tokens at least.
 struct Pages { int first, last; };
-__device__ __forceinline__ Pages pages_of(const Kv4View& c, const int32_t* __restrict__ table, int max_pages, int t0)
-{
-    const int first = kv4_page(table, max_pages, c.pages, c.shift, t0);
-    return Pages{first, c.shift > 4 ? first : kv4_page(table, max_pages, c.pages, c.shift, t0 + 16)};
-}
+// A sequence's row of the table, 64 entries in the lanes of a wavefront (-1: no page): a page is a read of a lane, and memory is asked once
+// in 64 pages.
+struct PageRow {
+    const int32_t* __restrict__ row;
+    int have = -1, entries = -1;           // which 64 of them; (per lane) the entry
+    __device__ __forceinline__ int page(const Kv4View& c, int max_pages, int t)
+    {
+        const int at = __builtin_amdgcn_readfirstlane(t >> c.shift);
+        if (at >> 6 != have) {
+            have = at >> 6;
+            entries = kv4_page(row, max_pages, c.pages, 0, 64 * have + (threadIdx.x & 63));
+        }
+        return __builtin_amdgcn_readlane(entries, at & 63);
+    }
+    __device__ __forceinline__ Pages pages(const Kv4View& c, int max_pages, int t0)
+    {
+        const int first = page(c, max_pages, t0);
+        return Pages{first, c.shift > 4 ? first : page(c, max_pages, t0 + 16)};
+    }
+};
 
 // 32 tokens of one head: where their rows are, and the grids of token 8 g + lane % 8.
 struct Where {
@@ -157,21 +173,27 @@ __device__ __forceinline__ void at_token(const Kv4View& c, const Where& w, bool 
     else f(second ? row1 : row0);
 }
 
+struct Grids {
+    uint32_t k, v;             // of token 8 g + lane % 8
+    bool first, last;          // whether the first and the last 16 tokens lie on a page
+};
+
 template <int D> struct Tokens {
     static constexpr int K = D / 32, V = D / 128 > 0 ? D / 128 : 1;   // words of a K row, words of a V row (dim 64: half a word)
     uint32_t k[2][K];
     uint32_t v[8][V];
-    uint32_t kg, vg;
-    bool first, last;
+    Grids grids;
 };
 
-__device__ __forceinline__ void load_grids(const Kv4View& c, const Where& w, uint32_t& kg, uint32_t& vg)
+__device__ __forceinline__ void load_grids(const Kv4View& c, const Where& w, Grids& x)
 {
+    x.first = w.first;
+    x.last = w.last;
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const unsigned at = 8 * g + (lane & 7);
     at_token(c, w, g & 2, [&](int64_t row) {
-        kg = (c.k_grids + row)[at];
-        vg = (c.v_grids + row)[at];
+        x.k = (c.k_grids + row)[at];
+        x.v = (c.v_grids + row)[at];
     });
 }
 
@@ -181,8 +203,6 @@ __device__ __forceinline__ void load_tokens(const Kv4View& c, Pages p, int h, in
     constexpr int ROW = D / 2;
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     const Where w = where(c, p, h, t0);
-    x.first = w.first;
-    x.last = w.last;
     // K: row r of instruction i is token 8 (r / 4) + 4 i + r % 4; V: row e of quarter g is token 8 g + e
     at_token(c, w, r & 8, [&](int64_t row) {
         const uint8_t* __restrict__ k = c.k_codes + row * ROW;
@@ -199,7 +219,7 @@ __device__ __forceinline__ void load_tokens(const Kv4View& c, Pages p, int h, in
             else __builtin_memcpy(x.v[e], __builtin_assume_aligned(v + off + e * ROW, 4 * Tokens<D>::V), sizeof x.v[e]);
         }
     });
-    load_grids(c, w, x.kg, x.vg);
+    load_grids(c, w, x.grids);
 }
 
 // What is taken off the values' codes, as fp16 with their offset: 1024 + zero for codes in the low half of a byte, 64 + zero (of
@@ -207,14 +227,15 @@ __device__ __forceinline__ void load_tokens(const Kv4View& c, Pages p, int h, in
 struct Zeros { h2 low[4], high[4]; };
 __device__ __forceinline__ Zeros value_zeros(uint32_t vg, const Bits& b)
 {
+    // a lane's own zero and its neighbour's (tokens 2 j and 2 j + 1 in lanes 2 j), then lane 2 j's to everybody
+    const uint32_t next = __builtin_amdgcn_mov_dpp(vg, 0xB1, 0xf, 0xf, true), both = __builtin_amdgcn_perm(next, vg, 0x05040100u);
+    const float low = __uint_as_float(and_or(both, LOW, b.h1024)), high = __uint_as_float(and_or(both << 4, HIGH, b.h64));
     Zeros z;
     for8([&](auto e) {
         constexpr int E = decltype(e)::value;
         if constexpr (E % 2 == 0) {
-            const uint32_t z0 = __builtin_amdgcn_mov_dpp(vg, 0x150 + E, 0xf, 0xf, true), z1 = __builtin_amdgcn_mov_dpp(vg, 0x151 + E, 0xf, 0xf, true);
-            const uint32_t both = __builtin_amdgcn_perm(z1, z0, 0x05040100u);
-            z.low[E / 2] = __builtin_bit_cast(h2, and_or(both, LOW, b.h1024));
-            z.high[E / 2] = __builtin_bit_cast(h2, and_or(both << 4, HIGH, b.h64));
+            z.low[E / 2] = __builtin_bit_cast(h2, from_lane<E>(low));
+            z.high[E / 2] = __builtin_bit_cast(h2, from_lane<E>(high));
         }
     });
     return z;
@@ -241,10 +262,10 @@ __device__ __forceinline__ u4 value_fragment(const uint32_t (&pair)[4], int n, c
 template <class T, int D, int QT, bool SHARE>
 __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
 {
-    constexpr int WAVES = 4, M = D / 16, TILE = 16 * QT * (SHARE ? 1 : WAVES);
+    constexpr int WAVES = 4, NT = 1, M = D / 16, TILE = 16 * QT * (SHARE ? 1 : WAVES);
     __shared__ __attribute__((aligned(16))) float sh_o[SHARE ? WAVES : 1][SHARE ? 16 * QT * (D + 4) : 4];
     __shared__ float sh_ml[SHARE ? WAVES : 1][SHARE ? 16 * QT * 2 : 1];
-    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : 2 * M][SHARE ? 1 : 64];   // fragments of K, then of V
+    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : NT * 2 * M][SHARE ? 1 : 64];   // per tile the fragments of K, then of V
 
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -314,7 +335,8 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         wg_from = a.q.window > 0 ? max(0, (a.q.causal ? before + first / G + 1 : length) - a.q.window) : 0;
     }
     const int tile0 = wg_from / 32, tile1 = (wg_to + 31) / 32;
-    const int per = max((max(0, tile1 - tile0) + a.parts - 1) / a.parts, KV4_PART / 32);
+    int per = max((max(0, tile1 - tile0) + a.parts - 1) / a.parts, KV4_PART / 32);
+    per = (per + NT - 1) / NT * NT;
     const int begin = tile0 + part * per, end = min(tile1, begin + per);
 
     f4 o[QT][M];
@@ -327,107 +349,134 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         for (int j = 0; j < M; ++j) o[t][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // one tile of tokens: its scores, weights and share of the sums.  key(i, k), value(u, n): the fragments
-    auto attend = [&](int t0, uint32_t kg, uint32_t vg, bool first, bool final, auto key, auto value) {
+    // NT tiles of tokens: their scores, weights and share of the sums.  key(x, i, k), value(x, u, n): the fragments of tile x
+    auto attend = [&](int t0, const Grids (&grids)[NT], auto key, auto value) {
         // a lane works on the grids of one token; the eight it needs come from the lanes of its quarter
-        const float ka = __uint_as_float(kg & 0xffff0000u) * a.scale2, kz = -(Frag<T>::OFFSET + (float)kv4_zero(kg));
-        const float va = __uint_as_float(vg & 0xffff0000u), vlog = (float)(max((int)(vg >> 23), 127 + VALUE_FLOOR) - 127);
-        float kas[8], vtop = vlog;
-        for8([&](auto e) {
-            constexpr int E = decltype(e)::value;
-            kas[E] = from_lane<E>(ka);
-            vtop = fmaxf(vtop, from_lane<E>(vlog));
-        });
-        f4 s[QT][2];
+        float va[NT], vlog[NT], kas[NT][8], vtop = VALUE_FLOOR;
+        f4 s[NT][QT][2];
+        bool whole = t0 >= all_from && t0 + 32 * NT <= all_to;
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
-            for8([&](auto e) { s[t][decltype(e)::value >> 2][decltype(e)::value & 3] = from_lane<decltype(e)::value>(kz) * qsum[t]; });
+        for (int x = 0; x < NT; ++x) {
+            const uint32_t kg = grids[x].k, vg = grids[x].v;
+            const float ka = __uint_as_float(kg & 0xffff0000u) * a.scale2, kz = -(Frag<T>::OFFSET + (float)kv4_zero(kg));
+            va[x] = __uint_as_float(vg & 0xffff0000u);
+            vlog[x] = (float)(max((int)(vg >> 23), 127 + VALUE_FLOOR) - 127);
+            whole = whole && grids[x].first && grids[x].last;
+            for8([&](auto e) {
+                constexpr int E = decltype(e)::value;
+                kas[x][E] = from_lane<E>(ka);
+                vtop = fmaxf(vtop, from_lane<E>(vlog[x]));
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+                for (int t = 0; t < QT; ++t) s[x][t][E >> 2][E & 3] = from_lane<E>(kz) * qsum[t];
+            });
+        }
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-                const u4 kf = key(i, k);
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-                for (int t = 0; t < QT; ++t) s[t][i] = Frag<T>::mfma(kf, qf[t][k], s[t][i]);
-            }
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < D / 32; ++k) {
+                    const u4 kf = key(x, i, k);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) s[x][t][i] = Frag<T>::mfma(kf, qf[t][k], s[x][t][i]);
+                }
         // u: scores above the running maximum, in binary orders
-        float u[QT][8], most = -INFINITY;
+        float u[NT][QT][8], most = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[t][e] = fmaf(s[t][e >> 2][e & 3], kas[e], -m[t]);
-        const bool edge = !(first && final && t0 >= all_from && t0 + 32 <= all_to);
-        if (edge) {
-            const bool page = (g & 2) ? final : first;
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
             for (int t = 0; t < QT; ++t)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int tok = t0 + 8 * g + e;
-                    if (tok < from[t] || tok >= to[t] || !page) u[t][e] = -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e) u[x][t][e] = fmaf(s[x][t][e >> 2][e & 3], kas[x][e], -m[t]);
+        if (!whole) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+                const bool page = (g & 2) ? grids[x].last : grids[x].first;
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int tok = t0 + 32 * x + 8 * g + e;
+                        if (tok < from[t] || tok >= to[t] || !page) u[x][t][e] = -INFINITY;
+                    }
+            }
         }
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, u[t][e]);
+            for (int t = 0; t < QT; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, u[x][t][e]);
         // no weight can pass 2^RAISE; where one might, the maximum is raised to what the tokens have
         if (__any(most + vtop > RAISE)) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
                 float z = -INFINITY;
-                for8([&](auto e) {
-                    constexpr int E = decltype(e)::value;
-                    if (u[t][E] != -INFINITY) {
-                        u[t][E] = s[t][E >> 2][E & 3] * kas[E];
-                        z = fmaxf(z, u[t][E] + from_lane<E>(vlog));
-                    }
-                });
+#pragma unroll
+                for (int x = 0; x < NT; ++x)
+                    for8([&](auto e) {
+                        constexpr int E = decltype(e)::value;
+                        const float log = from_lane<E>(vlog[x]);       // (all lanes take part)
+                        if (u[x][t][E] != -INFINITY) {
+                            u[x][t][E] = s[x][t][E >> 2][E & 3] * kas[x][E];
+                            z = fmaxf(z, u[x][t][E] + log);
+                        }
+                    });
                 const float up = fmaxf(m[t], quarters_max(z)), f = __builtin_amdgcn_exp2f(m[t] - up);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) u[t][e] -= up;
+                for (int x = 0; x < NT; ++x)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[x][t][e] -= up;
                 m[t] = up;
                 l[t] *= f;
 #pragma unroll
                 for (int j = 0; j < M; ++j) o[t][j] *= f;
             }
         }
-        f16x8 p[QT];
+        f16x8 p[NT][QT];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            float w[8];
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(u[t][e]);
-            l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-            for8([&](auto e) { p[t][decltype(e)::value] = (f16_t)(w[decltype(e)::value] * from_lane<decltype(e)::value>(va)); });
-        }
-        if (edge) {
+            for (int t = 0; t < QT; ++t) {
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(u[x][t][e]);
+                l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                for8([&](auto e) { p[x][t][decltype(e)::value] = (f16_t)(w[decltype(e)::value] * from_lane<decltype(e)::value>(va[x])); });
+            }
+        if (!whole) {
             // nothing also where the token's values are NaN
 #pragma unroll
-            for (int t = 0; t < QT; ++t)
+            for (int x = 0; x < NT; ++x)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (u[t][e] == -INFINITY) p[t][e] = (f16_t)0.f;
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (u[x][t][e] == -INFINITY) p[x][t][e] = (f16_t)0.f;
         }
 #pragma unroll
-        for (int n = 0; n < M; ++n) {
-            const u4 vf = value(n >> 2, n & 3);
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][n] = Frag<f16_t>::mfma(vf, __builtin_bit_cast(u4, p[t]), o[t][n]);
-        }
+            for (int n = 0; n < M; ++n) {
+                const u4 vf = value(x, n >> 2, n & 3);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) o[t][n] = Frag<f16_t>::mfma(vf, __builtin_bit_cast(u4, p[x][t]), o[t][n]);
+            }
     };
-    auto pages = [&](int i) { return pages_of(a.c, table, a.s.max_pages, (i < end ? i : begin) * 32); };
+    PageRow row_of_pages{table};
+    auto pages = [&](int tile) { return row_of_pages.pages(a.c, a.s.max_pages, tile * 32); };
     if constexpr (SHARE) {
-        // the pages two tiles ahead and the tokens of the next tile are on their way while a tile is attended to
+        // the tokens of the next tile are on their way while a tile is attended to
         int tile = begin + wave;
         if (tile < end) {
             using X = Tokens<D>;
             X x0, x1;
             auto use = [&](X& x) {
-                const Zeros z = value_zeros(x.vg, bits);
+                const Zeros z = value_zeros(x.grids.v, bits);
+                const Grids grids[1] = {x.grids};
                 uint32_t pair[4];
-                attend(tile * 32, x.kg, x.vg, x.first, x.last, [&](int i, int k) { return Frag<T>::codes(x.k[i][k], bits); },
-                       [&](int u, int n) {
+                attend(tile * 32, grids, [&](int, int i, int k) { return Frag<T>::codes(x.k[i][k], bits); },
+                       [&](int, int u, int n) {
                            if (n == 0)
 #pragma unroll
                                for (int j = 0; j < 4; ++j)
@@ -436,14 +485,11 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
                        });
             };
             load_tokens<D>(a.c, pages(tile), h, tile * 32, x0);
-            Pages next = pages(tile + WAVES);
             for (;;) {
-                if (tile + WAVES < end) load_tokens<D>(a.c, next, h, (tile + WAVES) * 32, x1);
-                next = pages(tile + 2 * WAVES);
+                if (tile + WAVES < end) load_tokens<D>(a.c, pages(tile + WAVES), h, (tile + WAVES) * 32, x1);
                 use(x0);
                 if ((tile += WAVES) >= end) break;
-                if (tile + WAVES < end) load_tokens<D>(a.c, next, h, (tile + WAVES) * 32, x0);
-                next = pages(tile + 2 * WAVES);
+                if (tile + WAVES < end) load_tokens<D>(a.c, pages(tile + WAVES), h, (tile + WAVES) * 32, x0);
                 use(x1);
                 if ((tile += WAVES) >= end) break;
             }
@@ -451,67 +497,73 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     } else if (begin < end) {
         // this wavefront's share of a tile: D / 64 fragments of K (numbers i D / 32 + k) and as many of V (4 u + n)
         constexpr int SHARE_OF = D / 64, ROW = D / 2;
-        struct Raw { uint32_t k[SHARE_OF], v[8], kg, vg; bool first, last; };
-        auto load = [&](Pages p, int t0, Raw& x) {
-            const Where w = where(a.c, p, h, t0);
-            const int r = col;
-            x.first = w.first;
-            x.last = w.last;
+        struct Raw { uint32_t k[NT][SHARE_OF]; us2 v[NT][4]; Grids grids[NT]; };   // v: the four channels of tokens 2 j and 2 j + 1
+        auto load = [&](int tile, Raw& raw) {
 #pragma unroll
-            for (int j = 0; j < SHARE_OF; ++j) {
-                const int f = wave * SHARE_OF + j, i = f / (D / 32), k = f % (D / 32);
-                at_token(a.c, w, r & 8, [&](int64_t row) {
-                    x.k[j] = *reinterpret_cast<const uint32_t*>(a.c.k_codes + row * ROW + ((8 * (r >> 2) + (r & 3) + 4 * i) * ROW + (D / 8) * g + 4 * k));
+            for (int x = 0; x < NT; ++x) {
+                const Where w = where(a.c, pages(tile + x), h, (tile + x) * 32);
+                const int r = col, u = (wave * SHARE_OF) >> 2;         // (all of a wavefront's fragments of V are of the same four channels)
+#pragma unroll
+                for (int j = 0; j < SHARE_OF; ++j) {
+                    const int f = wave * SHARE_OF + j, i = f / (D / 32), k = f % (D / 32);
+                    at_token(a.c, w, r & 8, [&](int64_t row) {
+                        raw.k[x][j] = *reinterpret_cast<const uint32_t*>(a.c.k_codes + row * ROW + (unsigned)((8 * (r >> 2) + (r & 3) + 4 * i) * ROW + (D / 8) * g + 4 * k));
+                    });
+                }
+                at_token(a.c, w, g & 2, [&](int64_t row) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        raw.v[x][e / 2][e & 1] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + (unsigned)((8 * g + e) * ROW + (D / 32) * r + 2 * u));
                 });
-            }
-            const int f = wave * SHARE_OF, u = f >> 2;                 // (all of a wavefront's fragments of V are of the same four channels)
-            at_token(a.c, w, g & 2, [&](int64_t row) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x.v[e] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + ((8 * g + e) * ROW + (D / 32) * r + 2 * u));
-            });
-            load_grids(a.c, w, x.kg, x.vg);
-        };
-        auto stage = [&](int buf, const Raw& x) {
-#pragma unroll
-            for (int j = 0; j < SHARE_OF; ++j) sh_f[buf][wave * SHARE_OF + j][lane] = Frag<T>::codes(x.k[j], bits);
-            const Zeros z = value_zeros(x.vg, bits);
-            uint32_t pair[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) pair[j] = x.v[2 * j] | x.v[2 * j + 1] << 16;
-            const int n0 = (wave * SHARE_OF) & 3;
-            if constexpr (SHARE_OF == 4) {
-#pragma unroll
-                for (int n = 0; n < 4; ++n) sh_f[buf][M + wave * 4 + n][lane] = value_fragment(pair, n, z, bits);
-            } else {
-                // the first channel is 0 or 2 (dim 128), or the wavefront's number (dim 64): the same for all lanes
-#pragma unroll
-                for (int n = 0; n < 4; ++n)
-                    if (n >= n0 && n < n0 + SHARE_OF) sh_f[buf][M + wave * SHARE_OF + n - n0][lane] = value_fragment(pair, n, z, bits);
+                load_grids(a.c, w, raw.grids[x]);
             }
         };
-        Raw x;
-        load(pages(begin), begin * 32, x);
-        Pages next = pages(begin + 1);
-        stage(0, x);
-        uint32_t kg = x.kg, vg = x.vg;
-        bool first = x.first, final = x.last;
-        if (begin + 1 < end) load(next, (begin + 1) * 32, x);
-        next = pages(begin + 2);
-        for (int tile = begin; tile < end; ++tile) {
-            const int buf = (tile - begin) & 1;
-            // this tile's fragments are in LDS, and everybody is done with the other buffer
+        auto stage = [&](int buf, const Raw& raw) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x) {
+#pragma unroll
+                for (int j = 0; j < SHARE_OF; ++j) sh_f[buf][x * 2 * M + wave * SHARE_OF + j][lane] = Frag<T>::codes(raw.k[x][j], bits);
+                const Zeros z = value_zeros(raw.grids[x].v, bits);
+                // from its first channel on: 0, 0 or 2 (dim 128), or the wavefront's number (dim 64); odd ones have their codes a half byte up
+                const int n0 = (wave * SHARE_OF) & 3;
+                uint32_t pair[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) pair[j] = __builtin_bit_cast(uint32_t, raw.v[x][j]) >> (D == 256 ? 0 : n0 & 2 ? 8 : 0);
+                u4* dst = &sh_f[buf][x * 2 * M + M + wave * SHARE_OF][lane];
+                if constexpr (SHARE_OF == 4) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) dst[n * 64] = value_fragment(pair, n, z, bits);
+                } else if constexpr (SHARE_OF == 2) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) dst[n * 64] = value_fragment(pair, n, z, bits);
+                } else {
+                    if (n0 & 1) dst[0] = value_fragment(pair, 1, z, bits);
+                    else dst[0] = value_fragment(pair, 0, z, bits);
+                }
+            }
+        };
+        Raw raw;
+        Grids grids[NT];
+        load(begin, raw);
+        stage(0, raw);
+#pragma unroll
+        for (int x = 0; x < NT; ++x) grids[x] = raw.grids[x];
+        if (begin + NT < end) load(begin + NT, raw);
+        for (int tile = begin; tile < end; tile += NT) {
+            const int buf = ((tile - begin) / NT) & 1;
+            // this step's fragments are in LDS, and everybody is done with the other buffer
             __syncthreads();
-            const uint32_t kg1 = x.kg, vg1 = x.vg;
-            const bool first1 = x.first, final1 = x.last;
-            if (tile + 1 < end) stage(buf ^ 1, x);
-            if (tile + 2 < end) load(next, (tile + 2) * 32, x);
-            next = pages(tile + 3);
+            Grids next[NT];
+#pragma unroll
+            for (int x = 0; x < NT; ++x) next[x] = raw.grids[x];
+            if (tile + NT < end) stage(buf ^ 1, raw);
+            if (tile + 2 * NT < end) load(tile + 2 * NT, raw);
             const int t0 = tile * 32;
-            if (t0 < any_to && t0 + 32 > any_from)
-                attend(t0, kg, vg, first, final, [&](int i, int k) { return sh_f[buf][i * (D / 32) + k][lane]; },
-                       [&](int u, int n) { return sh_f[buf][M + 4 * u + n][lane]; });
-            kg = kg1; vg = vg1; first = first1; final = final1;
+            if (t0 < any_to && t0 + 32 * NT > any_from)
+                attend(t0, grids, [&](int x, int i, int k) { return sh_f[buf][x * 2 * M + i * (D / 32) + k][lane]; },
+                       [&](int x, int u, int n) { return sh_f[buf][x * 2 * M + M + 4 * u + n][lane]; });
+#pragma unroll
+            for (int x = 0; x < NT; ++x) grids[x] = next[x];
         }
     }
 

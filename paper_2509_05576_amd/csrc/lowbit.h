@@ -36,7 +36,7 @@ hipError_t launch_fp8_from_codes(hipStream_t s, const uint8_t* codes, const floa
 
 // The product: tile edges and parts of the contraction (parts > 1: fp32 partial results in `work`, added by a second launch).
 struct Fp8Plan { int tm, tn, parts; int64_t blocks_per_part; };
-Fp8Plan fp8_matmul_plan(int cus, int64_t m, int64_t n, int64_t k, int type);
+Fp8Plan fp8_matmul_plan(int cus, int64_t m, int64_t n, int64_t k, int type, int per);
 int64_t fp8_matmul_workspace(const Fp8Plan& p, int64_t m, int64_t n);
 hipError_t launch_fp8_matmul(hipStream_t s, const Fp8Plan& p, const Fp8View& a, const Fp8View& b, void* y, int type, int64_t ldy, float* work);
 

@@ -231,6 +231,6 @@ def test_refusals(ctx):
         assert call(a, b, 4) == fobq.EINVAL, field
     big = fobq.binding._fp8(ctx.handle, m, "A")
     need = ctypes.c_int64(0)
-    assert lib.fobq_fp8_matmul_workspace(ctx.handle, 1, 128, 1 << 20, 1, ctypes.byref(need)) == fobq.OK and need.value > 0
+    assert lib.fobq_fp8_matmul_workspace(ctx.handle, 128, 128, 1 << 20, 1, ctypes.byref(need)) == fobq.OK and need.value > 0
     assert lib.fobq_fp8_matmul_workspace(ctx.handle, 1, -1, 128, 1, ctypes.byref(need)) == fobq.EINVAL
     torch.cuda.synchronize()

@@ -67,15 +67,17 @@ def test_places():
 
 @pytest.mark.parametrize("cus", [256, 64])
 @pytest.mark.parametrize("dtype", [0, 1, 2])
-def test_products_are_covered(cus, dtype):
+@pytest.mark.parametrize("per_scale", [1, 128])
+def test_products_are_covered(cus, dtype, per_scale):
     for m in (0, 1, 3, 16, 17, 64, 100, 1000, 8192, 100000):
         for n in (1, 16, 130, 4608, 8192):
             for k in (0, 1, 128, 129, 2304, 8192, 100000):
-                tm, tn, parts, per, work = plan(fobq.PLAN_FP8_MATMUL, [cus, m, n, k, dtype], 5)
+                tm, tn, parts, per, work = plan(fobq.PLAN_FP8_MATMUL, [cus, m, n, k, dtype, per_scale], 5)
                 blocks = -(-k // 128)
                 assert tm >= 1 and tn >= 1 and parts >= 1 and per >= 1
                 assert parts * per >= blocks and (parts - 1) * per < max(1, blocks)     # every block in one part, no part empty
                 assert work == (4 * parts * m * n if parts > 1 else 0)
+                assert work == plan(fobq.PLAN_FP8_MATMUL, [cus, m, n, k, dtype, 128], 5)[4]     # (asked for without the matrices)
                 # parts are for calls that do not fill the chip, and their results take little against the matrices
                 assert parts == 1 or -(-m // tm) * -(-n // tn) <= 2 * cus
 
