@@ -76,9 +76,9 @@ __device__ __forceinline__ auto operand(i8v x)
 
 // 16 bytes a lane from `offset` of a run of memory into LDS, lane after lane.  Behind the run's end nothing is read.
 typedef __amdgpu_buffer_rsrc_t Run;
-__device__ __forceinline__ Run run_of(const uint8_t* p, int64_t bytes)
+__device__ __forceinline__ Run run_of(const void* p, int64_t bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(uint32_t)min(bytes, (int64_t)0xffffffff), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)min(bytes, (int64_t)0xffffffff), 0x00020000);
 }
 __device__ __forceinline__ void copy16(Run run, unsigned offset, void* lds_base)
 {
@@ -185,36 +185,49 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
         for (int j = 0; j < SN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
     const int wm0 = wm * (TM / WM), wn0 = wn * (TN / WN);
-    // the scales of a block: one of A for each of this lane's rows; of B (in PER == 1) four for each of its column groups
+    // the scales of a block: one of A for each of this lane's rows; of B (in PER == 1) four for each of its column groups.  Behind the last
+    // row they read as zeros.
     struct Scales { float a[SM]; f4 b[PER == 1 ? SN : 1]; };
+    const unsigned sa_at = (wm0 + c) * 4, sb_at = (wn0 + 4 * q) * 4;
     auto scales = [&](int kb, Scales& s) {
+        const Run a = run_of(g.a.scales + kb * g.a.ld_scales + m0, (int64_t)(M - m0) * 4);
 #pragma unroll
-        for (int i = 0; i < SM; ++i) s.a[i] = g.a.scales[kb * g.a.ld_scales + min(m0 + wm0 + 16 * i + c, M - 1)];
+        for (int i = 0; i < SM; ++i) s.a[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(a, sa_at + 64 * i, 0, 0));
         if constexpr (PER == 1) {
+            const Run b = run_of(g.b.scales + kb * g.b.ld_scales + n0, (int64_t)(N - n0) * 4);
 #pragma unroll
             for (int j = 0; j < SN; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s.b[j][e] = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0 + 16 * j + 4 * q + e, N - 1)];
+                for (int e = 0; e < 4; ++e) s.b[j][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, sb_at + 64 * j + 4 * e, 0, 0));
         } else {
             s.b[0][0] = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0, N - 1) / 128];
         }
     };
+    // Rows of A in groups of 16, one behind the other: while the matrix instructions of a group run, the sums of the one before are added
+    // up and the next one's operand comes from LDS.  The order is kept; the compiler's own has every instruction wait for the one before.
     auto multiply = [&](int buf, const Scales& s) {
-        float sa[SM];
-#pragma unroll
-        for (int i = 0; i < SM; ++i) sa[i] = PER == 1 ? s.a[i] : s.a[i] * s.b[0][0];
-        decltype(operand<EXACT, FB>(i8v())) bf[SN];
+        using BF = decltype(operand<EXACT, FB>(i8v()));
+        using AF = decltype(operand<EXACT, FA>(i8v()));
+        BF bf[SN];
+        AF af[2];
+        f4 p[2][SN];
+        af[0] = operand<EXACT, FA>(fragment(buf, wm0));
 #pragma unroll
         for (int j = 0; j < SN; ++j) bf[j] = operand<EXACT, FB>(fragment(buf, TM + wn0 + 16 * j));
 #pragma unroll
-        for (int i = 0; i < SM; ++i) {
-            const auto af = operand<EXACT, FA>(fragment(buf, wm0 + 16 * i));
+        for (int i = 0; i <= SM; ++i) {
+            if (i + 1 < SM) af[(i + 1) & 1] = operand<EXACT, FA>(fragment(buf, wm0 + 16 * (i + 1)));
+            const float sa = i == 0 ? 0.f : PER == 1 ? s.a[i - 1] : s.a[i - 1] * s.b[0][0];
 #pragma unroll
             for (int j = 0; j < SN; ++j) {
-                f4 p = mfma_block<FB, FA>(bf[j], af);
-                if constexpr (PER == 1) p *= s.b[j];
+                if (i < SM) p[i & 1][j] = mfma_block<FB, FA>(bf[j], af[i & 1]);
+                if (i > 0) {
+                    f4& d = acc[i - 1][j];
+                    const f4 x = p[(i - 1) & 1][j];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], sa[i], acc[i][j][e]);
+                    for (int e = 0; e < 4; ++e) d[e] = fmaf(PER == 1 ? x[e] * s.b[PER == 1 ? j : 0][e] : x[e], sa, d[e]);
+                }
+                if (!EXACT) __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
