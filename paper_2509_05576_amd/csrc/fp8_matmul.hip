@@ -74,7 +74,7 @@ __device__ __forceinline__ auto operand(i8v x)
     else return x;
 }
 
-// 16 bytes a lane from `offset` of a run of memory into LDS, lane after lane.  Behind the run's end nothing is read.
+// 16 or 4 bytes a lane from `offset` of a run of memory into LDS, lane after lane.  Behind the run's end nothing is read.
 typedef __amdgpu_buffer_rsrc_t Run;
 __device__ __forceinline__ Run run_of(const void* p, int64_t bytes)
 {
@@ -83,6 +83,10 @@ __device__ __forceinline__ Run run_of(const void* p, int64_t bytes)
 __device__ __forceinline__ void copy16(Run run, unsigned offset, void* lds_base)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(run, (void __attribute__((address_space(3)))*)lds_base, 16, (int)offset, 0, 0, 0);
+}
+__device__ __forceinline__ void copy4(Run run, unsigned offset, void* lds_base)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(run, (void __attribute__((address_space(3)))*)lds_base, 4, (int)offset, 0, 0, 0);
 }
 
 // the place of a row's 16-byte piece
@@ -120,14 +124,25 @@ __device__ __forceinline__ void put4(const MatmulArgs& g, int part, int m, int n
     else out((f16_t)0.f);
 }
 
-constexpr int FEW_WAVES = 8;      // wavefronts of a workgroup for few rows
+constexpr int FEW_WAVES = 8, FEW_ROWS = 16;      // wavefronts of a workgroup for few rows of A, and how many those are
 
-// TM x TN outputs by WM x WN wavefronts.  FA, FB: the types of A and B; PER: rows of B to a scale.
-template <int TM, int TN, int WM, int WN, int FA, int FB, int PER, bool EXACT>
+// Waits until at most LEFT copies of this wavefront are under way, and for the whole workgroup to be there.  (A barrier of the language
+// waits for all of them.)
+template <int LEFT>
+__device__ __forceinline__ void wait_and_meet()
+{
+    static_assert(LEFT < 64, "a count of six bits");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
+// TM x TN outputs by WM x WN wavefronts, the tiles of STAGES - 1 blocks under way.  FA, FB: the types of A and B; PER: rows of B to a scale.
+template <int TM, int TN, int WM, int WN, int STAGES, int FA, int FB, int PER, bool EXACT>
 __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
 {
-    constexpr int THREADS = 64 * WM * WN, SM = TM / WM / 16, SN = TN / WN / 16;
-    __shared__ __attribute__((aligned(16))) uint8_t sh[2][(TM + TN) * 128];
+    constexpr int WAVES = WM * WN, THREADS = 64 * WAVES, SM = TM / WM / 16, SN = TN / WN / 16;
+    // per stage: rows of A, rows of B, and the scales of each
+    constexpr int ROWS = TM + TN, STAGE = ROWS * 132;
+    __shared__ __attribute__((aligned(16))) uint8_t sh[STAGES][STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, c = lane & 15;
     const int wm = wave / WN, wn = wave % WN;
@@ -147,16 +162,28 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
     const int row = threadIdx.x >> 3, column = swizzle(row, threadIdx.x & 7) * 16;
     const Run ra = run_of(g.a.values + m0 * g.a.ld, (M - m0) * g.a.ld), rb = run_of(g.b.values + n0 * g.b.ld, (N - n0) * g.b.ld);
     const unsigned lda = (unsigned)g.a.ld, ldb = (unsigned)g.b.ld, oa = row * lda + column, ob = row * ldb + column;
-    auto fetch = [&](int buf, int kb) {
+    auto fetch_values = [&](int stage, int kb) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) copy16(ra, oa + (i * STEP) * lda + (unsigned)kb * 128, &sh[buf][(i * THREADS + wave * 64) * 16]);
+        for (int i = 0; i < PA; ++i) copy16(ra, oa + (i * STEP) * lda + (unsigned)kb * 128, &sh[stage][(i * THREADS + wave * 64) * 16]);
 #pragma unroll
-        for (int i = 0; i < PB; ++i) copy16(rb, ob + (i * STEP) * ldb + (unsigned)kb * 128, &sh[buf][TM * 128 + (i * THREADS + wave * 64) * 16]);
+        for (int i = 0; i < PB; ++i) copy16(rb, ob + (i * STEP) * ldb + (unsigned)kb * 128, &sh[stage][TM * 128 + (i * THREADS + wave * 64) * 16]);
     };
+    // A block's scales, one for each row of A and of B: 64 a wavefront.  (With fewer of them than wavefronts some are copied twice.)
+    static_assert(ROWS / 64 == WAVES || WAVES % (ROWS / 64) == 0, "every wavefront copies scales once");
+    const int piece = wave % (ROWS / 64);
+    const bool of_a = piece < TM / 64;
+    const int scale0 = of_a ? m0 : n0 / PER, scales_there = of_a ? M - m0 : (N + PER - 1) / PER - scale0;
+    const unsigned scale_at = of_a ? piece * 64 + lane : (n0 + piece * 64 - TM + lane) / PER - scale0;
+    const float* const scale_of = (of_a ? g.a.scales : g.b.scales) + scale0;
+    const int64_t scale_ld = of_a ? g.a.ld_scales : g.b.ld_scales;
+    auto fetch_scales = [&](int stage, int kb) {
+        copy4(run_of(scale_of + kb * scale_ld, (int64_t)scales_there * 4), scale_at * 4, &sh[stage][ROWS * 128 + piece * 256]);
+    };
+    constexpr int COPIES = PA + PB + 1;
     // the last block of columns where it is not whole: what is behind it counts as zero, whatever the rows hold there
-    auto fetch_rest = [&](int buf, int kb) {
+    auto fetch_rest = [&](int stage, int kb) {
         const int k = kb * 128 + column, left = K - k;
-        auto piece = [&](const Fp8View& x, int at, int rows, uint8_t* dst) {
+        auto put = [&](const Fp8View& x, int at, int rows, uint8_t* dst) {
             uint32_t w[4] = {0, 0, 0, 0};
             if (left > 0 && at < rows) {
                 __builtin_memcpy(w, __builtin_assume_aligned(x.values + at * x.ld + k, 16), 16);
@@ -168,12 +195,12 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
             }
             __builtin_memcpy(__builtin_assume_aligned(dst, 16), w, 16);
         };
-        for (int i = 0; i < PA; ++i) piece(g.a, m0 + i * STEP + row, M, &sh[buf][(i * THREADS + threadIdx.x) * 16]);
-        for (int i = 0; i < PB; ++i) piece(g.b, n0 + i * STEP + row, N, &sh[buf][TM * 128 + (i * THREADS + threadIdx.x) * 16]);
+        for (int i = 0; i < PA; ++i) put(g.a, m0 + i * STEP + row, M, &sh[stage][(i * THREADS + threadIdx.x) * 16]);
+        for (int i = 0; i < PB; ++i) put(g.b, n0 + i * STEP + row, N, &sh[stage][TM * 128 + (i * THREADS + threadIdx.x) * 16]);
     };
     const int p0 = swizzle(c, 2 * q) * 16, p1 = swizzle(c, 2 * q + 1) * 16;
-    auto fragment = [&](int buf, int first_row) {
-        const uint8_t* p = &sh[buf][(first_row + c) * 128];
+    auto fragment = [&](int stage, int first_row) {
+        const uint8_t* p = &sh[stage][(first_row + c) * 128];
         const i4 lo = *reinterpret_cast<const i4*>(p + p0), hi = *reinterpret_cast<const i4*>(p + p1);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
@@ -185,39 +212,31 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
         for (int j = 0; j < SN; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
     const int wm0 = wm * (TM / WM), wn0 = wn * (TN / WN);
-    // the scales of a block: one of A for each of this lane's rows; of B (in PER == 1) four for each of its column groups.  Behind the last
-    // row they read as zeros.
-    struct Scales { float a[SM]; f4 b[PER == 1 ? SN : 1]; };
-    const unsigned sa_at = (wm0 + c) * 4, sb_at = (wn0 + 4 * q) * 4;
-    auto scales = [&](int kb, Scales& s) {
-        const Run a = run_of(g.a.scales + kb * g.a.ld_scales + m0, (int64_t)(M - m0) * 4);
-#pragma unroll
-        for (int i = 0; i < SM; ++i) s.a[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(a, sa_at + 64 * i, 0, 0));
-        if constexpr (PER == 1) {
-            const Run b = run_of(g.b.scales + kb * g.b.ld_scales + n0, (int64_t)(N - n0) * 4);
-#pragma unroll
-            for (int j = 0; j < SN; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s.b[j][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, sb_at + 64 * j + 4 * e, 0, 0));
-        } else {
-            s.b[0][0] = g.b.scales[kb * g.b.ld_scales + min(n0 + wn0, N - 1) / 128];
-        }
-    };
     // Rows of A in groups of 16, one behind the other: while the matrix instructions of a group run, the sums of the one before are added
     // up and the next one's operand comes from LDS.  The order is kept; the compiler's own has every instruction wait for the one before.
-    auto multiply = [&](int buf, const Scales& s) {
+    auto multiply = [&](int stage) {
         using BF = decltype(operand<EXACT, FB>(i8v()));
         using AF = decltype(operand<EXACT, FA>(i8v()));
+        const float* scales = reinterpret_cast<const float*>(&sh[stage][ROWS * 128]);
         BF bf[SN];
         AF af[2];
-        f4 p[2][SN];
-        af[0] = operand<EXACT, FA>(fragment(buf, wm0));
+        f4 p[2][SN], sb[PER == 1 ? SN : 1];
+        float sa[SM];
+        af[0] = operand<EXACT, FA>(fragment(stage, wm0));
 #pragma unroll
-        for (int j = 0; j < SN; ++j) bf[j] = operand<EXACT, FB>(fragment(buf, TM + wn0 + 16 * j));
+        for (int j = 0; j < SN; ++j) bf[j] = operand<EXACT, FB>(fragment(stage, TM + wn0 + 16 * j));
+#pragma unroll
+        for (int i = 0; i < SM; ++i) sa[i] = scales[wm0 + 16 * i + c];
+        if constexpr (PER == 1) {
+#pragma unroll
+            for (int j = 0; j < SN; ++j) sb[j] = *reinterpret_cast<const f4*>(&scales[TM + wn0 + 16 * j + 4 * q]);
+        } else {
+            sb[0][0] = scales[TM + wn0];
+        }
 #pragma unroll
         for (int i = 0; i <= SM; ++i) {
-            if (i + 1 < SM) af[(i + 1) & 1] = operand<EXACT, FA>(fragment(buf, wm0 + 16 * (i + 1)));
-            const float sa = i == 0 ? 0.f : PER == 1 ? s.a[i - 1] : s.a[i - 1] * s.b[0][0];
+            if (i + 1 < SM) af[(i + 1) & 1] = operand<EXACT, FA>(fragment(stage, wm0 + 16 * (i + 1)));
+            const float s = i == 0 ? 0.f : PER == 1 ? sa[i - 1] : sa[i - 1] * sb[0][0];
 #pragma unroll
             for (int j = 0; j < SN; ++j) {
                 if (i < SM) p[i & 1][j] = mfma_block<FB, FA>(bf[j], af[i & 1]);
@@ -225,36 +244,38 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
                     f4& d = acc[i - 1][j];
                     const f4 x = p[(i - 1) & 1][j];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[e] = fmaf(PER == 1 ? x[e] * s.b[PER == 1 ? j : 0][e] : x[e], sa, d[e]);
+                    for (int e = 0; e < 4; ++e) d[e] = fmaf(PER == 1 ? x[e] * sb[PER == 1 ? j : 0][e] : x[e], s, d[e]);
                 }
                 if (!EXACT) __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
     const int whole = min(kb1, K / 128);                     // blocks of this part that are whole
-    Scales next;
-    if (kb0 < whole) {
-        scales(kb0, next);
-        fetch(0, kb0);
-    }
-    for (int kb = kb0; kb < whole; ++kb) {
-        const int buf = (kb - kb0) & 1;
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        const Scales s = next;
-        // (in this order: the scales would otherwise be waited for behind the copies, which are not needed until the next block)
-        if (kb + 1 < whole) {
-            scales(kb + 1, next);
-            fetch(buf ^ 1, kb + 1);
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+        if (kb0 + k < whole) {
+            fetch_values(k, kb0 + k);
+            fetch_scales(k, kb0 + k);
         }
-        multiply(buf, s);
+    int stage = 0;
+    for (int kb = kb0; kb < whole; ++kb) {
+        if (kb + STAGES - 2 < whole) wait_and_meet<(STAGES - 2) * COPIES>();
+        else wait_and_meet<0>();
+        // everybody is done with the block before: its stage is free
+        if (kb + STAGES - 1 < whole) {
+            const int free = stage == 0 ? STAGES - 1 : stage - 1;
+            fetch_values(free, kb + STAGES - 1);
+            fetch_scales(free, kb + STAGES - 1);
+        }
+        multiply(stage);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
     }
     if (whole < kb1) {
-        __syncthreads();
+        wait_and_meet<0>();
         fetch_rest(0, whole);
-        scales(whole, next);
-        __syncthreads();
-        multiply(0, next);
+        fetch_scales(0, whole);
+        wait_and_meet<0>();
+        multiply(0);
     }
 #pragma unroll
     for (int i = 0; i < SM; ++i) {
@@ -268,24 +289,20 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
     }
 }
 
-// Few rows of A: the weights are read once, straight into the registers of the wavefront that multiplies them, 128 bytes of 16 rows in
+// Up to 16 rows of A: the weights are read once, straight into the registers of the wavefront that multiplies them, 128 bytes of 16 rows in
 // two loads.  A workgroup has 16 rows of B; its wavefronts deal the blocks among them, four at a time (8 KiB of weights in flight each), and
 // add up in LDS, in their order.  On fp16 values throughout: conversions are hidden behind memory.
-template <int MT, int FA, int FB, int PER>
+template <int FA, int FB, int PER>
 __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_matmul_few_kernel(MatmulArgs g)
 {
-    constexpr int AT_ONCE = MT == 1 ? 4 : 2;
-    __shared__ f4 sum[FEW_WAVES][MT][64];
+    constexpr int AT_ONCE = 4;
+    __shared__ f4 sum[FEW_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
     const int M = g.a.rows, N = g.b.rows, K = g.a.cols, blocks = (K + 127) / 128;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
+    const int n0 = blockIdx.x * 16;
     const uint8_t* __restrict__ brow = g.b.values + (int64_t)min(n0 + c, N - 1) * g.b.ld + 32 * q;
-    const uint8_t* __restrict__ arow[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) arow[i] = g.a.values + (int64_t)min(m0 + 16 * i + c, M - 1) * g.a.ld + 32 * q;
-    f4 acc[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = f4{0.f, 0.f, 0.f, 0.f};
+    const uint8_t* __restrict__ arow = g.a.values + (int64_t)min(c, M - 1) * g.a.ld + 32 * q;
+    f4 acc = {0.f, 0.f, 0.f, 0.f};
 
     auto load = [&](const uint8_t* __restrict__ row, int kb) {
         i4 lo, hi;
@@ -313,17 +330,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_matmul_few_kernel(MatmulAr
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     for (int kb0 = wave * AT_ONCE; kb0 < blocks; kb0 += FEW_WAVES * AT_ONCE) {
-        i8v b[AT_ONCE], a[AT_ONCE][MT];
-        float sa[AT_ONCE][MT], sb[AT_ONCE][PER == 1 ? 4 : 1];
+        i8v b[AT_ONCE], a[AT_ONCE];
+        float sa[AT_ONCE], sb[AT_ONCE][PER == 1 ? 4 : 1];
 #pragma unroll
         for (int x = 0; x < AT_ONCE; ++x) {
             b[x] = load(brow, kb0 + x);
             const int kb = min(kb0 + x, blocks - 1);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                a[x][i] = load(arow[i], kb0 + x);
-                sa[x][i] = g.a.scales[kb * g.a.ld_scales + min(m0 + 16 * i + c, M - 1)];
-            }
+            a[x] = load(arow, kb0 + x);
+            sa[x] = g.a.scales[kb * g.a.ld_scales + min(c, M - 1)];
             if constexpr (PER == 1) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sb[x][e] = g.b.scales[kb * g.b.ld_scales + min(n0 + 4 * q + e, N - 1)];
@@ -334,24 +348,19 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_matmul_few_kernel(MatmulAr
 #pragma unroll
         for (int x = 0; x < AT_ONCE; ++x) {
             if (kb0 + x >= blocks) break;
-            const auto bf = as_fp16<FB>(b[x]);
+            const f4 p = mfma_block<FB, FA>(as_fp16<FB>(b[x]), as_fp16<FA>(a[x]));
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const f4 p = mfma_block<FB, FA>(bf, as_fp16<FA>(a[x][i]));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(p[e] * sb[x][PER == 1 ? e : 0], sa[x][i], acc[i][e]);
-            }
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(p[e] * sb[x][PER == 1 ? e : 0], sa[x], acc[e]);
         }
     }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sum[wave][i][lane] = acc[i];
+    sum[wave][lane] = acc;
     __syncthreads();
-    if (wave < MT) {
-        f4 v = sum[0][wave][lane];
+    if (wave == 0) {
+        f4 v = sum[0][lane];
 #pragma unroll
-        for (int k = 1; k < FEW_WAVES; ++k) v += sum[k][wave][lane];
-        const int m = m0 + 16 * wave + c, n = n0 + 4 * q;
-        if (m < M && n < N) put4(g, 0, m, n, v);
+        for (int k = 1; k < FEW_WAVES; ++k) v += sum[k][lane];
+        const int n = n0 + 4 * q;
+        if (c < M && n < N) put4(g, 0, c, n, v);
     }
 }
 
@@ -380,21 +389,30 @@ __global__ __launch_bounds__(256) void fp8_matmul_join_kernel(MatmulArgs g)
     put4(whole, 0, (int)m, n, sum);
 }
 
+// The measurements behind the rules (bf16 results, a scale per 128 x 128, us; n = k = 8192 where one number is given):
+//   up to 16 rows         one kernel for few rows: 13.2 with 1 row; with 17 and 32 rows 21 and 26 against 16 and 17 in tiles of 64
+//   64, 128 or 256        1024 rows 136, 89, 104; 2048 rows 262, 169, 127; 300 x 4608 x 2048 10.8, 16.8, 33; 2000^3 26, 21, 35;
+//                         4096^3 134, 91, 65; 1500 x 6000 x 3000 65, 55, 50.  A compute unit has one workgroup of the largest tiles at a
+//                         time or two of the others, and the larger of two takes less per value, 1 : 1.4
+//   parts of the sum      64 rows, 128 tiles of 64 blocks: 25 in one part, 19 in two and in four; 128 rows, 256 tiles: 26 and 27;
+//                         500 x 1000 x 2304, 18 blocks: 10 and 14 (the second launch takes 4.5)
 Fp8Plan fp8_matmul_plan(int cus, int64_t m, int64_t n, int64_t k, int type, int per)
 {
     Fp8Plan p;
-    if (m <= 32) {
-        p.tm = m <= 16 ? 16 : 32;
-        p.tn = 16;
-        p.parts = 1;
-        p.blocks_per_part = std::max<int64_t>(1, (k + 127) / 128);
-        return p;
+    const int64_t blocks = (k + 127) / 128;
+    auto tiles = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
+    auto rounds = [&](int64_t t, int64_t at_once) { return (tiles(t) + at_once - 1) / at_once; };
+    int64_t want = 1;
+    if (m <= FEW_ROWS) {
+        p.tm = p.tn = FEW_ROWS;
+    } else if (type != FOBQ_F32 && per == 128 && 10 * rounds(256, cus) <= 7 * rounds(128, 2 * cus)) {
+        p.tm = p.tn = 256;              // (results in 32 bits, or a scale per row of B, take more registers than there are)
+    } else if (tiles(128) >= cus) {
+        p.tm = p.tn = 128;
+    } else {
+        p.tm = p.tn = 64;
+        if (tiles(64) < cus) want = std::max<int64_t>(1, std::min(2 * cus / std::max<int64_t>(1, tiles(64)), blocks / 16));
     }
-    // 256 x 256 tiles where they fill the chip; with results in 32 bits, or a scale per row of B, their operands do not fit the registers
-    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
-    p.tm = p.tn = type != FOBQ_F32 && per == 128 && large >= cus ? 256 : 128;
-    const int64_t tiles = std::max<int64_t>(1, ((m + p.tm - 1) / p.tm) * ((n + p.tn - 1) / p.tn)), blocks = (k + 127) / 128;
-    const int64_t want = std::min<int64_t>(std::max<int64_t>(1, cus / tiles), std::max<int64_t>(1, blocks / 4));
     p.blocks_per_part = std::max<int64_t>(1, (blocks + want - 1) / want);
     p.parts = (int)std::max<int64_t>(1, (blocks + p.blocks_per_part - 1) / p.blocks_per_part);
     return p;
@@ -406,16 +424,20 @@ template <int FA, int FB, int PER>
 static hipError_t matmul_of(hipStream_t s, const Fp8Plan& p, const MatmulArgs& g)
 {
     const dim3 grid((unsigned)(((g.a.rows + p.tm - 1) / p.tm) * ((g.b.rows + p.tn - 1) / p.tn)), (unsigned)p.parts);
-    if (p.tn == 16) {
-        const dim3 few((unsigned)((g.b.rows + 15) / 16), (unsigned)((g.a.rows + p.tm - 1) / p.tm)), block(64 * FEW_WAVES);
-        if (p.tm == 16) hipLaunchKernelGGL((fp8_matmul_few_kernel<1, FA, FB, PER>), few, block, 0, s, g);
-        else hipLaunchKernelGGL((fp8_matmul_few_kernel<2, FA, FB, PER>), few, block, 0, s, g);
+    if (p.tm == FEW_ROWS) {
+        hipLaunchKernelGGL((fp8_matmul_few_kernel<FA, FB, PER>), dim3((unsigned)((g.b.rows + 15) / 16)), dim3(64 * FEW_WAVES), 0, s, g);
         return hipGetLastError();
     }
-    if (g.type == FOBQ_F32) hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
-    else if (p.tm == 256) {
-        if constexpr (PER == 128) hipLaunchKernelGGL((fp8_matmul_kernel<256, 256, 2, 4, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
-    } else hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+    const bool exact = g.type == FOBQ_F32;
+    if (p.tm == 256) {
+        if constexpr (PER == 128) hipLaunchKernelGGL((fp8_matmul_kernel<256, 256, 2, 4, 2, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
+    } else if (p.tm == 128) {
+        if (exact) hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, 2, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
+        else hipLaunchKernelGGL((fp8_matmul_kernel<128, 128, 2, 2, 2, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+    } else {
+        if (exact) hipLaunchKernelGGL((fp8_matmul_kernel<64, 64, 2, 2, 4, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
+        else hipLaunchKernelGGL((fp8_matmul_kernel<64, 64, 2, 2, 4, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     const int64_t items = (int64_t)g.a.rows * ((g.b.rows + 3) / 4);

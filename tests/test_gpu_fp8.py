@@ -102,7 +102,7 @@ def test_from_codes_is_the_layer(ctx, r, d, bits, group):
 
 
 SIZES = [(1, 1, 1), (1, 64, 128), (1, 1000, 2047), (5, 33, 130), (16, 256, 4608), (17, 130, 384), (64, 512, 1024), (100, 129, 257),
-         (129, 257, 640), (256, 256, 512), (300, 1000, 2304), (513, 300, 100)]
+         (129, 257, 640), (256, 256, 512), (300, 1000, 2304), (513, 300, 100), (40, 100, 5000), (2100, 2300, 300), (2100, 2301, 300), (4000, 4100, 260)]
 
 
 @pytest.mark.parametrize("per", [1, 128])
