@@ -573,29 +573,45 @@ class Kv4Batch:
 
 def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
     """What the library calls a cache and a batch."""
-    k, v = _need(cache.k_codes, ctx, _U8, 4, "k_codes"), _need(cache.v_codes, ctx, _U8, 4, "v_codes")
-    kg, vg = _need(cache.k_grids, ctx, _I32, 3, "k_grids"), _need(cache.v_grids, ctx, _I32, 3, "v_grids")
-    shape = k.shape
-    pages, heads, page, half = shape
-    if v.shape != shape or kg.shape != shape[:3] or vg.shape != shape[:3] or not (
-            k.is_contiguous() and v.is_contiguous() and kg.is_contiguous() and vg.is_contiguous()):
-        raise TypeError(f"cache: need contiguous codes {tuple(shape)} and grids {tuple(shape[:3])}, got v_codes {tuple(v.shape)}, "
-                        f"k_grids {tuple(kg.shape)}, v_grids {tuple(vg.shape)}")
-    table, lengths, starts = _need(batch.table, ctx, _I32, 2, "table"), _need(batch.lengths, ctx, _I32, 1, "lengths"), batch.starts
-    n, width = table.shape
-    if lengths.shape[0] != n:
-        raise TypeError(f"lengths: need {n} entries, got {lengths.shape[0]}")
-    if starts is not None and _need(starts, ctx, _I32, 1, "starts").shape[0] != n + 1:
-        raise TypeError(f"starts: need {n + 1} entries, got {starts.shape[0]}")
+    k, v, kg, vg, table, lengths, starts = cache.k_codes, cache.v_codes, cache.k_grids, cache.v_grids, batch.table, batch.lengths, batch.starts
+    home, u8, i32 = _streams.get(ctx), torch.uint8, torch.int32
+    dev = home[0] if home is not None else None
+    try:
+        shape = k.shape
+        n, width = table.shape
+        pages, heads, page, half = shape
+        grid = kg.shape
+        fine = (k.dtype is u8 and v.dtype is u8 and kg.dtype is i32 and vg.dtype is i32 and table.dtype is i32 and lengths.dtype is i32
+                and k.get_device() == dev and v.get_device() == dev and kg.get_device() == dev and vg.get_device() == dev
+                and table.get_device() == dev and lengths.get_device() == dev and v.shape == shape and grid == shape[:3] and vg.shape == grid
+                and k.is_contiguous() and v.is_contiguous() and kg.is_contiguous() and vg.is_contiguous()
+                and (table.stride(1) == 1 or width <= 1) and lengths.shape == (n,) and lengths.is_contiguous()
+                and (starts is None or (starts.dtype is i32 and starts.get_device() == dev and starts.shape == (n + 1,) and starts.is_contiguous())))
+    except (AttributeError, ValueError):
+        fine = False
+    if not fine:
+        # which of them it is
+        _need(k, ctx, _U8, 4, "k_codes")
+        for name, t, dtypes, dims in (("v_codes", v, _U8, 4), ("k_grids", kg, _I32, 3), ("v_grids", vg, _I32, 3)):
+            _need(t, ctx, dtypes, dims, name)
+        if v.shape != k.shape or kg.shape != k.shape[:3] or vg.shape != k.shape[:3] or not all(t.is_contiguous() for t in (k, v, kg, vg)):
+            raise TypeError(f"cache: need contiguous codes {tuple(k.shape)} and grids {tuple(k.shape[:3])}, got v_codes {tuple(v.shape)}, "
+                            f"k_grids {tuple(kg.shape)}, v_grids {tuple(vg.shape)}")
+        n = _need(table, ctx, _I32, 2, "table").shape[0]
+        if _need(lengths, ctx, _I32, 1, "lengths").shape[0] != n:
+            raise TypeError(f"lengths: need {n} entries, got {lengths.shape[0]}")
+        if starts is not None and _need(starts, ctx, _I32, 1, "starts").shape[0] != n + 1:
+            raise TypeError(f"starts: need {n + 1} entries, got {starts.shape[0]}")
+        pages, heads, page, half = k.shape
+        width = table.shape[1]
     return (FobqKv4Cache(k.data_ptr(), v.data_ptr(), kg.data_ptr(), vg.data_ptr(), pages, page, heads, 2 * half, 0),
             FobqKv4Batch(table.data_ptr(), lengths.data_ptr(), starts.data_ptr() if starts is not None else None, rows,
                          table.stride(0) if n > 1 else width, n, width))
 
 
 def _kv_rows(ctx: int, c: FobqKv4Cache, k: torch.Tensor, v: torch.Tensor, rows: int, dtypes):
-    _need(k, ctx, dtypes, 3, "k")
+    shape = _need(k, ctx, dtypes, 3, "k").shape
     _need(v, ctx, dtypes, 3, "v")
-    shape = k.shape
     if v.shape != shape or k.dtype != v.dtype or shape[0] != rows or shape[1] != c.heads or shape[2] != c.head_dim:
         raise TypeError(f"k and v: need {(rows, c.heads, c.head_dim)} of one type, got {tuple(shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
     return (_FLOAT[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1))

@@ -222,12 +222,13 @@ int hip_err(fobq_ctx* c, hipError_t e, const char* what);
 struct DeviceGuard {
     int prev = -1;
     bool ok = true;
-    explicit DeviceGuard(int dev)
+    int dev;
+    explicit DeviceGuard(int dev_) : dev(dev_)
     {
         if (hipGetDevice(&prev) != hipSuccess) prev = -1;
         if (prev != dev) ok = (hipSetDevice(dev) == hipSuccess);
     }
-    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
+    ~DeviceGuard() { if (prev >= 0 && prev != dev) (void)hipSetDevice(prev); }
 };
 
 // Timing of a stage that is exactly one launch: the two events ride on the launch as its start and stop

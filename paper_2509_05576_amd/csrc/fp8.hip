@@ -3,9 +3,9 @@
 //
 // A block's scale is its largest magnitude over the type's largest value (e4m3 448, e5m2 57344), at least 2^-126 (which a block of
 // zeros has); the values are the nearest ones to x / scale, ties to even.  A block that holds an Inf or NaN is NaN throughout.
-// The quotient: with top = 0.875 * 2^9 or * 2^16, x / (most / top) = (0.875 x) / (most / 2^9 or 2^16), whose operands are exact for 16-bit x;
-// one multiplication by the reciprocal and one correction from the remainder round it as a division would, so that a quotient on the border
-// of two 8-bit values is seen as one.  It never passes the largest value by more than a rounding, which the conversion takes back.
+// The quotient: with top = 0.875 * 2^9 or * 2^16, x / (most / top) = (0.875 x) / (most / 2^9 or 2^16); one multiplication by the reciprocal
+// and one correction from the remainder round it as a division would, so that a quotient on the border of two 8-bit values is seen as one.  It
+// never passes the largest value by more than a rounding, which the conversion takes back.
 #include "lowbit.h"
 
 namespace fobq {
@@ -41,11 +41,11 @@ __device__ __forceinline__ Fp8Scale fp8_scale(uint32_t bits)
     const float m = most * Fp8<FORMAT>::POW, inv = 1.f / m;
     return Fp8Scale{scale, 0.875f, m, inv, inv};
 }
-// x / scale
+// x / scale, rounded once: the remainder of the first guess is exact (its product's error is taken along, and what is left of x fits)
 __device__ __forceinline__ float fp8_quotient(const Fp8Scale& s, float x)
 {
-    const float t = x * s.pre, y = t * s.inv;
-    return fmaf(fmaf(-y, s.most, t), s.corr, y);
+    const float y = x * s.pre * s.inv, p = y * s.most, e = fmaf(y, s.most, -p);
+    return fmaf(fmaf(x, s.pre, -p) - e, s.corr, y);
 }
 
 // 8 values into 8 bytes of a row, or those of them that the row has
@@ -56,14 +56,19 @@ __device__ __forceinline__ void put8(uint8_t* __restrict__ dst, int left, const 
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = fp8_quotient(s, x[i]);
     const uint32_t w[2] = {to_fp8x4<FORMAT>(y[0], y[1], y[2], y[3]), to_fp8x4<FORMAT>(y[4], y[5], y[6], y[7])};
-    if (left >= 8) __builtin_memcpy(dst, w, 8);
-    else
-        for (int i = 0; i < left; ++i) dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    if (left >= 8) {
+        __builtin_memcpy(dst, w, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
 }
 template <class T>
 __device__ __forceinline__ void get8(const T* __restrict__ src, int left, float* x)
 {
     if (left >= 8) { load8(src, x); return; }
+#pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = i < left ? (float)src[i] : 0.f;
 }
 // the largest magnitude as its bits, which order as the magnitudes do, Inf and NaN above all others
@@ -76,15 +81,25 @@ __device__ __forceinline__ uint32_t most8(const float* x)
 }
 __device__ __forceinline__ uint32_t other(uint32_t m, int off) { return (uint32_t)__shfl_xor((int)m, off); }
 
+// Item first + i of rows of `pieces` items: its row and its place there.  `first` is the workgroup's: one 64-bit division for all of its
+// threads, and a 32-bit one each.
+struct Item { int64_t row; int piece; };
+__device__ __forceinline__ Item item_of(int64_t first, unsigned i, unsigned pieces)
+{
+    const int64_t row = first / pieces;
+    const unsigned at = (unsigned)(first - row * pieces) + i, rows = at / pieces;
+    return Item{row + rows, (int)(at - rows * pieces)};
+}
+
 // A scale per row: 16 lanes have a block, 8 columns each; a wavefront four consecutive blocks of a row.
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void fp8_rows_kernel(const T* __restrict__ x, int64_t ld, Fp8View out)
 {
     const int lane = threadIdx.x & 63;
-    const int blocks = (out.cols + 127) / 128, quads = (blocks + 3) / 4;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t row = item / quads;
-    const int col = (int)(item - row * quads) * 512 + 8 * lane, left = out.cols - col;
+    const unsigned quads = (out.cols + 511) / 512;
+    const Item at = item_of((int64_t)blockIdx.x * 4, threadIdx.x >> 6, quads);
+    const int64_t row = at.row;
+    const int col = at.piece * 512 + 8 * lane, left = out.cols - col;
     if (row >= out.rows) return;
     float v[8];
     get8(x + row * ld + col, left, v);
@@ -128,30 +143,36 @@ __global__ __launch_bounds__(256) void fp8_tiles_kernel(const T* __restrict__ x,
 }
 
 // The codes of a layer (Section 3: q = scale (code - zero)): code - zero is an integer of at most 15 in magnitude for codes of up to
-// four bits, which e4m3 holds exactly, and the grid's scale is the block's.  16 codes a thread.
+// four bits, which e4m3 holds exactly, and the grid's scale is the block's.  16 codes a thread; the last workgroups turn the scales from
+// rows x groups into blocks x rows, a row a lane (written beside the codes, one word in a line at a time, they took longer than those).
 __global__ __launch_bounds__(256) void fp8_codes_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales, const float* __restrict__ zeros,
-                                                        int groups, int group, Fp8View out)
+                                                        int groups, int group, unsigned code_wgs, Fp8View out)
 {
-    const int pieces = (out.cols + 15) / 16;
-    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = item / pieces;
-    const int col = (int)(item - row * pieces) * 16, left = out.cols - col;
+    if (blockIdx.x >= code_wgs) {
+        const Item at = item_of((int64_t)(blockIdx.x - code_wgs) * 256, threadIdx.x, out.rows);
+        const int64_t kb = at.row;
+        if (kb * 128 < out.cols) out.scales[kb * out.ld_scales + at.piece] = scales[(int64_t)at.piece * groups + (group ? kb * 128 / group : 0)];
+        return;
+    }
+    const Item at = item_of((int64_t)blockIdx.x * 256, threadIdx.x, (out.cols + 15) / 16);
+    const int64_t row = at.row;
+    const int col = at.piece * 16, left = out.cols - col;
     if (row >= out.rows) return;
-    const int64_t g = row * groups + (group ? col / group : 0);
-    const float zero = zeros[g];
-    if (col % 128 == 0) out.scales[(int64_t)(col / 128) * out.ld_scales + row] = scales[g];
+    const float zero = zeros[row * groups + (group ? col / group : 0)];
     const uint8_t* __restrict__ src = codes + row * out.cols + col;
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (left >= 16) __builtin_memcpy(w, src, 16);
-    else
-        for (int i = 0; i < left; ++i) w[i >> 2] |= (uint32_t)src[i] << (8 * (i & 3));
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        w[k] = to_fp8x4<FOBQ_E4M3>((float)(w[k] & 255u) - zero, (float)(w[k] >> 8 & 255u) - zero, (float)(w[k] >> 16 & 255u) - zero, (float)(w[k] >> 24) - zero);
     uint8_t* dst = out.values + row * out.ld + col;
-    if (left >= 16) __builtin_memcpy(dst, w, 16);
-    else
-        for (int i = 0; i < left; ++i) dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    auto four = [&](uint32_t w) {
+        return to_fp8x4<FOBQ_E4M3>((float)(w & 255u) - zero, (float)(w >> 8 & 255u) - zero, (float)(w >> 16 & 255u) - zero, (float)(w >> 24) - zero);
+    };
+    if (left >= 16) {
+        uint32_t w[4];
+        __builtin_memcpy(w, src, 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = four(w[k]);
+        __builtin_memcpy(dst, w, 16);
+    } else {
+        for (int i = 0; i < left; ++i) dst[i] = (uint8_t)four(src[i]);
+    }
 }
 
 template <class T, int FORMAT>
@@ -177,8 +198,10 @@ hipError_t launch_fp8_quantize(hipStream_t s, const void* x, int type, int64_t l
 
 hipError_t launch_fp8_from_codes(hipStream_t s, const uint8_t* codes, const float* scales, const float* zeros, int group, const Fp8View& out)
 {
-    const int64_t items = (int64_t)out.rows * ((out.cols + 15) / 16);
-    hipLaunchKernelGGL(fp8_codes_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, codes, scales, zeros, group ? out.cols / group : 1, group, out);
+    const int64_t pieces = (int64_t)out.rows * ((out.cols + 15) / 16), blocks = (int64_t)out.rows * ((out.cols + 127) / 128);
+    const unsigned code_wgs = (unsigned)((pieces + 255) / 256);
+    hipLaunchKernelGGL(fp8_codes_kernel, dim3(code_wgs + (unsigned)((blocks + 255) / 256)), dim3(256), 0, s, codes, scales, zeros,
+                       group ? out.cols / group : 1, group, code_wgs, out);
     return hipGetLastError();
 }
 

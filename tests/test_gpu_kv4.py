@@ -290,6 +290,49 @@ def test_without_starts(ctx):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+def test_without_starts_rows_behind_the_last_sequence_stay(ctx):
+    for rows in (5, 5000):
+        c = Case(ctx, [(70, 1), (5, 1), (33, 1)], 2, 128, 16, seed=12)
+        before = [t.clone() for t in (c.cache.k_codes, c.cache.v_codes, c.cache.k_grids, c.cache.v_grids)]
+        kv = torch.randn((rows, 4, 128), generator=c.g).to(BF).cuda()
+        kv[:3, :2], kv[:3, 2:] = (torch.stack([x[j][-1] for x in c.kv]).cuda() for j in range(2))     # what is there already
+        ctx.kv4_append(c.cache, c.batch(starts=None), kv[:, :2], kv[:, 2:])
+        assert all(torch.equal(a, b) for a, b in zip(before, (c.cache.k_codes, c.cache.v_codes, c.cache.k_grids, c.cache.v_grids)))
+        out = tuple(torch.full((rows, 2, 128), 4.0, device="cuda") for _ in range(2))
+        k, v = ctx.kv4_read(c.cache, c.batch(starts=None), rows, out=out)
+        assert (k[3:] == 4).all() and (v[3:] == 4).all() and not (k[:3] == 4).any()
+        q = torch.randn((rows, 4, 128), generator=c.g).to(BF).cuda()
+        o = torch.full((rows, 4, 128), 4.0, dtype=BF, device="cuda")
+        ctx.kv4_attention(c.cache, c.batch(starts=None), q, out=o)
+        assert (o[3:] == 4).all()
+        c.check(q[:3].cpu(), o[:3], ctx_lse(ctx, c, q[:3]), 128 ** -0.5)
+
+
+def ctx_lse(ctx, c, q):
+    lse = torch.zeros((q.shape[0], q.shape[1]), device="cuda")
+    ctx.kv4_attention(c.cache, c.batch(starts=None), q, lse=lse)
+    return lse
+
+
+def test_many_rows_of_many_sequences(ctx):
+    """More rows than a wavefront each: sequences that end inside a group of four, empty ones between them."""
+    g = torch.Generator().manual_seed(2)
+    seqs = []
+    while sum(n for n, _ in seqs) < 5000:
+        n = int(torch.randint(0, 90, (1,), generator=g))
+        seqs.append((n, min(n, int(torch.randint(0, 5, (1,), generator=g)))))
+    c = Case(ctx, seqs, 1, 64, 16, seed=3)
+    k, v = ctx.kv4_read(c.cache, c.all, c.tokens, torch.float32)
+    at = 0
+    for s, (n, _) in enumerate(c.seqs):
+        for j, (got, (level, scale)) in enumerate(zip((k, v), c.rows_of(s))):
+            assert torch.equal(got[at:at + n].cpu(), (level * scale[..., None]).transpose(0, 1).float())
+            codes, want_scale, zero = ref.grid(c.kv[s][j].transpose(0, 1))
+            assert torch.equal(scale, want_scale) and torch.equal(level, codes - zero[..., None])
+        at += n
+    run(c, 2)
+
+
 def test_the_hint_of_the_longest_changes_no_coverage(ctx):
     c = Case(ctx, [(3000, 1)], 1, 128, 64, seed=13)
     for longest in (0, 1, 500, 3000, 1 << 20):
