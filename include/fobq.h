@@ -446,7 +446,8 @@ int fobq_debug_offset_tables(int32_t k, int32_t pad, int64_t h, int64_t w, int32
  *   FOBQ_PLAN_FP8_MATMUL  in: compute units, m, n, k, type of the result (fobq_float), rows of B to a scale
  *                  out: rows of A and of B of a tile, parts of the contraction, blocks of 128 a part, bytes of work
  *   FOBQ_PLAN_KV4_ATTENTION  in: compute units, head_dim, heads, group, n_seqs, rows, longest sequence
- *                  out: query rows of a workgroup, whether its wavefronts share them, parts of the tokens, workgroups a head and part, bytes of work
+ *                  out: query rows of a workgroup, whether its wavefronts share them, workgroups of a head where sequences are split (0: they are
+ *                  not), workgroups of a head that hold all rows, bytes of work
  *   FOBQ_PLAN_KV4_PLACE  in: page_size, pages, max_pages, n_seqs, rows, a packed row, then lengths (n_seqs), starts (n_seqs + 1), table (n_seqs x max_pages)
  *                  out: the sequence, page and place that the row's token has (page -1: none)
  *   FOBQ_PLAN_FP8_CHECK  in: rows, cols, ld, ld_scales, rows_per_scale, format, values, scales (addresses that are not followed)

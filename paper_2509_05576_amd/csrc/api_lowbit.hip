@@ -93,8 +93,7 @@ int lowbit_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* ou
         if (in[0] < 16 || in[0] > 4096 || (in[1] != 64 && in[1] != 128 && in[1] != 256) || in[2] < 1 || in[2] > 1024 || in[3] < 1 || in[3] > 1024 || in[4] < 1 ||
             in[4] > (1 << 20) || in[5] < 0 || in[5] * in[2] * in[3] >= MAX_SIDE || in[6] < 0 || in[6] >= ((int64_t)1 << 30)) return FOBQ_EINVAL;
         const Kv4Plan p = kv4_attention_plan((int)in[0], (int)in[1], (int)in[2], (int)in[3], (int)in[4], in[5], in[6]);
-        out[0] = p.tile; out[1] = p.share; out[2] = p.parts; out[3] = p.tiles;
-        out[4] = kv4_attention_workspace(p, (int)in[1], (int)in[2], (int)in[3], in[5]);
+        out[0] = p.tile; out[1] = p.share; out[2] = p.slots; out[3] = p.tiles; out[4] = kv4_attention_workspace(p, (int)in[1], (int)in[2]);
         return FOBQ_OK;
     }
     if (what == FOBQ_PLAN_KV4_PLACE && n_in >= 6 && n_out == 3) {
@@ -260,7 +259,7 @@ int fobq_kv4_attention_workspace(fobq_ctx* ctx, const fobq_kv4_cache* cache, con
     Kv4Plan p;
     const int rc = check_attention(ctx, cache, batch, query, &c, &s, &p);
     if (rc) return rc;
-    *bytes = kv4_attention_workspace(p, c.dim, c.heads, query->group, s.rows);
+    *bytes = kv4_attention_workspace(p, c.dim, c.heads);
     return FOBQ_OK;
 }
 
@@ -275,7 +274,7 @@ int fobq_kv4_attention(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv
     if (s.rows == 0 || s.n_seqs == 0) return FOBQ_OK;
     if (!query->Q || !query->out || !aligned(query->Q, 2) || !aligned(query->out, 2) || !aligned(query->lse, 4))
         return set_err(ctx, FOBQ_EINVAL, "Q or out is NULL, or Q, out or lse is not aligned to its elements");
-    const int64_t need = kv4_attention_workspace(p, c.dim, c.heads, query->group, s.rows);
+    const int64_t need = kv4_attention_workspace(p, c.dim, c.heads);
     if (work_bytes < need || (need > 0 && (!work || !aligned(work, 16))))
         return set_err(ctx, FOBQ_EINVAL, "work must be %lld bytes, 16-byte aligned (got %lld)", (long long)need, (long long)work_bytes);
     DeviceGuard g(ctx->device);

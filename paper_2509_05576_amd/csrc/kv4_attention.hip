@@ -13,9 +13,10 @@
 // K are dealt to the instruction's rows accordingly.  V's row n is the n-th piece of dim / 16 channels of a token, read as that, and
 // the lane transposes 8 tokens x dim / 16 codes by byte selects.  A lane's results are dim / 4 consecutive channels of one query row.
 //
-// fp16 weights and the range of V: m is the running maximum of S + log2 scale_v (its whole part), not of S, so that a row's largest weights
-// are near 1 whatever the size of the values.  The sum of the softmax has the same m and takes any size in fp32; values below 2^-88
-// count as that large there, which keeps it finite.
+// fp16 weights and the range of V: m follows the running maximum of S + log2 scale_v (its whole part), not of S, so that a row's largest
+// weights are near 1 whatever the size of the values.  The sum of the softmax has the same m, raised by 2^28 (scale_v takes that off P again):
+// with scales up to 2^127 its largest terms are still 2^27 times what fp32 can hold, with scales down to 2^-60 2^31 of them are finite.
+// Smaller scales count as 2^-60 in m, so that values below 2^-74 lose bits.
 // The maximum is raised only when it is exceeded by 2^8: most tiles of 32 tokens then rescale nothing.
 #include "kv4.h"
 
@@ -32,19 +33,110 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 
 constexpr float NEG_MAX = -3.402823466e38f;
-constexpr int VALUE_FLOOR = -88;
+constexpr int VALUE_FLOOR = -60;
+constexpr float BIAS = 28.f, BIAS2 = 268435456.f;       // and 2^BIAS
 constexpr float RAISE = 8.f;            // binary orders of magnitude that a score may exceed the running maximum by
 constexpr int KV4_PART = 256;           // tokens of a part at least: eight tiles, two for each wavefront that shares the rows
+// Sequences of no more tokens than these are not split: one launch, not two, and no scratch.  (8 of 600 tokens, from call to call: 13 us,
+// 18 split; 32 of 1024: 16, 19.  At 2048 it turns: 16 sequences 20 us either way, 8 with 8 new tokens each 24, 19 split.)
+constexpr int KV4_UNSPLIT = 1024;
 constexpr int KV4_MAX_PARTS = 64;       // a lane each where they are joined
+constexpr int KV4_SPLIT_SEQS = 256;     // more sequences than these are not split: they fill the chip
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 
 struct AttnArgs {
     Kv4View c; Kv4Seqs s; Kv4Query q;
-    int parts, heads_q;
+    int heads_q, tile;     // query heads; query rows of a workgroup
+    int slots;             // workgroups of a head where sequences are split (0: none is)
     float scale2;          // scale * log2(e)
-    float* part_o;         // parts x rows x query heads x dim
-    float* part_ml;        // the same without dim: maximum (in binary orders) and sum
+    float* part_o;         // heads x slots x tile x dim: sums of the rows of a split sequence's part
+    float* part_ml;        // the same without dim: maximum (in binary orders) and sum of the weights
 };
+
+// How the sequences are split into parts of about equal size, which the host cannot know: the lengths are on the device.  A sequence has
+// one workgroup per tile of its rows and part of its tokens; the longest part is as short as it can be with all of them in the slots
+// that there are, which the chip holds at a time.  Every wavefront works this out for itself, a lane to a sequence.  (32 sequences of 5000 to
+// 16000 tokens in as many parts each take 88 us, so 82; 8 of 16384 in three times as many parts 48, so 40.)
+struct Split {
+    static constexpr int J = KV4_SPLIT_SEQS / 64;
+    int row[J], count[J], length[J], parts[J], first[J], items[J];   // of sequence 64 j + lane: its packed rows, its tokens, its parts; its
+                                                                     // slots are first .. first + items - 1
+};
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+// the sum over the lanes up to this one
+__device__ __forceinline__ int sum_to_lane(int x)
+{
+    x = add_dpp<0x111, 0xf>(x);              // the lane below in a row of 16, two, four, eight below
+    x = add_dpp<0x112, 0xf>(x);
+    x = add_dpp<0x114, 0xf>(x);
+    x = add_dpp<0x118, 0xf>(x);
+    x = add_dpp<0x142, 0xa>(x);              // the last lane of the row below, to the second and fourth row
+    return add_dpp<0x143, 0xc>(x);           // of the second row, to the upper half
+}
+__device__ __forceinline__ Split split_of(const AttnArgs& a)
+{
+    constexpr int J = Split::J;
+    const int lane = threadIdx.x & 63;
+    Split s;
+    int tiles[J], spans[J], low = 0, high = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int b = 64 * j + lane;
+        s.row[j] = s.count[j] = s.length[j] = tiles[j] = spans[j] = 0;
+        if (64 * j < a.s.n_seqs && b < a.s.n_seqs) {
+            const Kv4Rows r = kv4_rows(a.s.starts, b, a.s.rows);
+            s.row[j] = r.first;
+            s.count[j] = r.count;
+            s.length[j] = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
+            const int tokens = a.q.window > 0 ? (int)min((int64_t)s.length[j], (int64_t)a.q.window + r.count) : s.length[j];
+            tiles[j] = (r.count * a.q.group + a.tile - 1) / a.tile;
+            spans[j] = (tokens + 31) / 32;
+            // (starts out of order could make more tiles than there are slots: those are cut off, here and where they are joined)
+            const uint64_t work = (uint64_t)min(tiles[j], a.slots) * spans[j];       // below 2^17 * 2^25
+            low += (int)(work & 0xffff);
+            high += (int)(work >> 16);
+        }
+    }
+    low = __builtin_amdgcn_readlane(sum_to_lane(low), 63);
+    high = __builtin_amdgcn_readlane(sum_to_lane(high), 63);
+    const float total = (float)high * 65536.f + (float)low;
+    // parts of sequence 64 j + lane if none is longer than `span` tiles of 32 tokens
+    auto parts_at = [&](int j, int span) { return max(1, min(KV4_MAX_PARTS, (int)((unsigned)(spans[j] + span - 1) / (unsigned)span))); };
+    auto fits = [&](int span) {
+        int sum = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (64 * j < a.s.n_seqs) sum += min(tiles[j], a.slots) * parts_at(j, span);
+        return __builtin_amdgcn_readlane(sum_to_lane(sum), 63) <= a.slots;
+    };
+    int all = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) all += min(tiles[j], a.slots);
+    const int spare = a.slots - __builtin_amdgcn_readlane(sum_to_lane(all), 63);
+    // between the whole work over all slots, and over those that are left when every tile has one (which always fits)
+    int span = spare > 0 ? (int)fminf(total / (float)spare * 1.000001f + 2.f, 1e9f) : 1 << 30, below = (int)(total / (float)a.slots) - 1;
+    span = max(span, KV4_PART / 32);
+    below = max(below, KV4_PART / 32 - 1);
+    for (int i = 0; i < 6 && below + 1 < span; ++i) {
+        const int mid = below + (span - below) / 2;
+        if (fits(mid)) span = mid;
+        else below = mid;
+    }
+    int before = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        s.parts[j] = 1;
+        s.items[j] = s.first[j] = 0;
+        if (64 * j >= a.s.n_seqs) continue;
+        s.parts[j] = parts_at(j, span);
+        s.items[j] = min(tiles[j], a.slots) * s.parts[j];
+        const int sum = sum_to_lane(s.items[j]);
+        s.first[j] = before + sum - s.items[j];
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return s;
+}
 
 // (x & mask) | bits is one instruction where the compiler has the mask in a scalar register and the bits in a vector one; as two
 // literals they cost an instruction each.  So the bits are made where it cannot see what they are.  (The instruction itself is left to the
@@ -262,29 +354,51 @@ __device__ __forceinline__ u4 value_fragment(const uint32_t (&pair)[4], int n, c
 template <class T, int D, int QT, bool SHARE>
 __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
 {
-    constexpr int WAVES = 4, NT = 1, M = D / 16, TILE = 16 * QT * (SHARE ? 1 : WAVES);
+    constexpr int WAVES = 4, M = D / 16, TILE = 16 * QT * (SHARE ? 1 : WAVES);
     __shared__ __attribute__((aligned(16))) float sh_o[SHARE ? WAVES : 1][SHARE ? 16 * QT * (D + 4) : 4];
     __shared__ float sh_ml[SHARE ? WAVES : 1][SHARE ? 16 * QT * 2 : 1];
-    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : NT * 2 * M][SHARE ? 1 : 64];   // per tile the fragments of K, then of V
+    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : 2 * M][SHARE ? 1 : 64];   // fragments of K, then of V
 
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int G = a.q.group;
     const Bits bits = offset_bits();
 
-    // the sequence and the rows of this workgroup: sequence b's tiles begin at floor(first row * G / TILE) + b, which leaves room for
-    // every sequence's last, partial tile
-    auto first_tile = [&](int b) { return (int64_t)kv4_rows(a.s.starts, b, a.s.rows).first * G / TILE + b; };
-    // (few rows: in their order; many: the last ones first, which see most)
-    const int h = blockIdx.x % a.c.heads, place = blockIdx.x / a.c.heads, index = SHARE ? place : (int)(gridDim.x / a.c.heads) - 1 - place;
-    const int b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, index, first_tile));
-    const Kv4Rows mine = kv4_rows(a.s.starts, b, a.s.rows);
+    // the sequence, the tile of its rows and the part of its tokens that this workgroup has
+    const int h = blockIdx.x % a.c.heads, index = blockIdx.x / a.c.heads;
+    int b = -1, part = 0, parts = 1, tile_of_rows = 0, length = 0;
+    Kv4Rows mine{0, 0};
+    if (a.slots) {
+        const Split split = split_of(a);
+#pragma unroll
+        for (int j = 0; j < Split::J; ++j) {
+            const uint64_t hit = __ballot(index >= split.first[j] && index < split.first[j] + split.items[j]);
+            if (hit) {
+                const int at = __ffsll((unsigned long long)hit) - 1;
+                b = 64 * j + at;
+                mine = Kv4Rows{__builtin_amdgcn_readlane(split.row[j], at), __builtin_amdgcn_readlane(split.count[j], at)};
+                length = __builtin_amdgcn_readlane(split.length[j], at);
+                parts = __builtin_amdgcn_readlane(split.parts[j], at);
+                const int i = index - __builtin_amdgcn_readlane(split.first[j], at);
+                tile_of_rows = i / parts;
+                part = i - tile_of_rows * parts;
+            }
+        }
+        if (b < 0) return;
+    } else {
+        // sequence b's tiles begin at floor(first row * G / TILE) + b, which leaves room for every sequence's last, partial tile; with
+        // many rows the last tiles first, which see most
+        auto first_tile = [&](int i) { return (int64_t)kv4_rows(a.s.starts, i, a.s.rows).first * G / TILE + i; };
+        const int place = SHARE ? index : (int)(gridDim.x / a.c.heads) - 1 - index;
+        b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, place, first_tile));
+        mine = kv4_rows(a.s.starts, b, a.s.rows);
+        length = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
+        tile_of_rows = (int)max((int64_t)-1, place - first_tile(b));
+    }
     const int rows = mine.count * G;                                   // tokens x query heads of the kv head
-    const int64_t base64 = (index - first_tile(b)) * TILE;
+    const int64_t base64 = (int64_t)tile_of_rows * TILE;
     if (base64 < 0 || base64 >= rows) return;
     const int base = (int)base64 + (SHARE ? 0 : wave * 16 * QT);
-    const int part = blockIdx.y;
-    const int length = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
     const int before = length - mine.count;                            // position of the sequence's first new token (< 0: it is not there)
     const int32_t* __restrict__ table = a.s.table + (int64_t)b * a.s.table_ld;
 
@@ -335,8 +449,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         wg_from = a.q.window > 0 ? max(0, (a.q.causal ? before + first / G + 1 : length) - a.q.window) : 0;
     }
     const int tile0 = wg_from / 32, tile1 = (wg_to + 31) / 32;
-    int per = max((max(0, tile1 - tile0) + a.parts - 1) / a.parts, KV4_PART / 32);
-    per = (per + NT - 1) / NT * NT;
+    const int per = (max(0, tile1 - tile0) + parts - 1) / parts;
     const int begin = tile0 + part * per, end = min(tile1, begin + per);
 
     f4 o[QT][M];
@@ -349,119 +462,94 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         for (int j = 0; j < M; ++j) o[t][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // NT tiles of tokens: their scores, weights and share of the sums.  key(x, i, k), value(x, u, n): the fragments of tile x
-    auto attend = [&](int t0, const Grids (&grids)[NT], auto key, auto value) {
+    // 32 tokens: their scores, weights and share of the sums.  key(i, k), value(u, n): the fragments
+    auto attend = [&](int t0, const Grids& grids, auto key, auto value) {
         // a lane works on the grids of one token; the eight it needs come from the lanes of its quarter
-        float va[NT], vlog[NT], kas[NT][8], vtop = VALUE_FLOOR;
-        f4 s[NT][QT][2];
-        bool whole = t0 >= all_from && t0 + 32 * NT <= all_to;
+        const float ka = __uint_as_float(grids.k & 0xffff0000u) * a.scale2, kz = -(Frag<T>::OFFSET + (float)kv4_zero(grids.k));
+        const float va = __uint_as_float(grids.v & 0xffff0000u) * (1.f / BIAS2), vlog = (float)(max((int)(grids.v >> 23), 127 + VALUE_FLOOR) - 127);
+        float kas[8], vtop = VALUE_FLOOR;
+        f4 s[QT][2];
+        for8([&](auto e) {
+            constexpr int E = decltype(e)::value;
+            kas[E] = from_lane<E>(ka);
+            vtop = fmaxf(vtop, from_lane<E>(vlog));
 #pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const uint32_t kg = grids[x].k, vg = grids[x].v;
-            const float ka = __uint_as_float(kg & 0xffff0000u) * a.scale2, kz = -(Frag<T>::OFFSET + (float)kv4_zero(kg));
-            va[x] = __uint_as_float(vg & 0xffff0000u);
-            vlog[x] = (float)(max((int)(vg >> 23), 127 + VALUE_FLOOR) - 127);
-            whole = whole && grids[x].first && grids[x].last;
-            for8([&](auto e) {
-                constexpr int E = decltype(e)::value;
-                kas[x][E] = from_lane<E>(ka);
-                vtop = fmaxf(vtop, from_lane<E>(vlog[x]));
+            for (int t = 0; t < QT; ++t) s[t][E >> 2][E & 3] = from_lane<E>(kz) * qsum[t];
+        });
 #pragma unroll
-                for (int t = 0; t < QT; ++t) s[x][t][E >> 2][E & 3] = from_lane<E>(kz) * qsum[t];
-            });
-        }
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+            for (int k = 0; k < D / 32; ++k) {
+                const u4 kf = key(i, k);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) {
-                    const u4 kf = key(x, i, k);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) s[x][t][i] = Frag<T>::mfma(kf, qf[t][k], s[x][t][i]);
-                }
-        // u: scores above the running maximum, in binary orders
-        float u[NT][QT][8], most = -INFINITY;
-#pragma unroll
-        for (int x = 0; x < NT; ++x)
-#pragma unroll
-            for (int t = 0; t < QT; ++t)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[x][t][e] = fmaf(s[x][t][e >> 2][e & 3], kas[x][e], -m[t]);
-        if (!whole) {
-#pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                const bool page = (g & 2) ? grids[x].last : grids[x].first;
-#pragma unroll
-                for (int t = 0; t < QT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int tok = t0 + 32 * x + 8 * g + e;
-                        if (tok < from[t] || tok >= to[t] || !page) u[x][t][e] = -INFINITY;
-                    }
+                for (int t = 0; t < QT; ++t) s[t][i] = Frag<T>::mfma(kf, qf[t][k], s[t][i]);
             }
-        }
+        // u: scores above the running maximum, in binary orders
+        float u[QT][8], most = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[t][e] = fmaf(s[t][e >> 2][e & 3], kas[e], -m[t]);
+        const bool whole = grids.first && grids.last && t0 >= all_from && t0 + 32 <= all_to;
+        if (!whole) {
+            const bool page = (g & 2) ? grids.last : grids.first;
 #pragma unroll
             for (int t = 0; t < QT; ++t)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, u[x][t][e]);
-        // no weight can pass 2^RAISE; where one might, the maximum is raised to what the tokens have
-        if (__any(most + vtop > RAISE)) {
+                for (int e = 0; e < 8; ++e) {
+                    const int tok = t0 + 8 * g + e;
+                    if (tok < from[t] || tok >= to[t] || !page) u[t][e] = -INFINITY;
+                }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, u[t][e]);
+        // no P can pass 2^RAISE; where one might, the maximum is raised to what the tokens have
+        if (__any(most + vtop > BIAS + RAISE)) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
                 float z = -INFINITY;
+                for8([&](auto e) {
+                    constexpr int E = decltype(e)::value;
+                    const float log = from_lane<E>(vlog);              // (all lanes take part)
+                    if (u[t][E] != -INFINITY) {
+                        u[t][E] = s[t][E >> 2][E & 3] * kas[E];
+                        z = fmaxf(z, u[t][E] + log);
+                    }
+                });
+                const float up = fmaxf(m[t], quarters_max(z) - BIAS), f = __builtin_amdgcn_exp2f(m[t] - up);
 #pragma unroll
-                for (int x = 0; x < NT; ++x)
-                    for8([&](auto e) {
-                        constexpr int E = decltype(e)::value;
-                        const float log = from_lane<E>(vlog[x]);       // (all lanes take part)
-                        if (u[x][t][E] != -INFINITY) {
-                            u[x][t][E] = s[x][t][E >> 2][E & 3] * kas[x][E];
-                            z = fmaxf(z, u[x][t][E] + log);
-                        }
-                    });
-                const float up = fmaxf(m[t], quarters_max(z)), f = __builtin_amdgcn_exp2f(m[t] - up);
-#pragma unroll
-                for (int x = 0; x < NT; ++x)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[x][t][e] -= up;
+                for (int e = 0; e < 8; ++e) u[t][e] -= up;
                 m[t] = up;
                 l[t] *= f;
 #pragma unroll
                 for (int j = 0; j < M; ++j) o[t][j] *= f;
             }
         }
-        f16x8 p[NT][QT];
+        f16x8 p[QT];
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+        for (int t = 0; t < QT; ++t) {
+            float w[8];
 #pragma unroll
-            for (int t = 0; t < QT; ++t) {
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(u[x][t][e]);
-                l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-                for8([&](auto e) { p[x][t][decltype(e)::value] = (f16_t)(w[decltype(e)::value] * from_lane<decltype(e)::value>(va[x])); });
-            }
+            for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(u[t][e]);
+            l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            for8([&](auto e) { p[t][decltype(e)::value] = (f16_t)(w[decltype(e)::value] * from_lane<decltype(e)::value>(va)); });
+        }
         if (!whole) {
             // nothing also where the token's values are NaN
 #pragma unroll
-            for (int x = 0; x < NT; ++x)
+            for (int t = 0; t < QT; ++t)
 #pragma unroll
-                for (int t = 0; t < QT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (u[x][t][e] == -INFINITY) p[x][t][e] = (f16_t)0.f;
+                for (int e = 0; e < 8; ++e)
+                    if (u[t][e] == -INFINITY) p[t][e] = (f16_t)0.f;
         }
 #pragma unroll
-        for (int x = 0; x < NT; ++x)
+        for (int n = 0; n < M; ++n) {
+            const u4 vf = value(n >> 2, n & 3);
 #pragma unroll
-            for (int n = 0; n < M; ++n) {
-                const u4 vf = value(x, n >> 2, n & 3);
-#pragma unroll
-                for (int t = 0; t < QT; ++t) o[t][n] = Frag<f16_t>::mfma(vf, __builtin_bit_cast(u4, p[x][t]), o[t][n]);
-            }
+            for (int t = 0; t < QT; ++t) o[t][n] = Frag<f16_t>::mfma(vf, __builtin_bit_cast(u4, p[t]), o[t][n]);
+        }
     };
     PageRow row_of_pages{table};
     auto pages = [&](int tile) { return row_of_pages.pages(a.c, a.s.max_pages, tile * 32); };
@@ -473,10 +561,9 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
             X x0, x1;
             auto use = [&](X& x) {
                 const Zeros z = value_zeros(x.grids.v, bits);
-                const Grids grids[1] = {x.grids};
                 uint32_t pair[4];
-                attend(tile * 32, grids, [&](int, int i, int k) { return Frag<T>::codes(x.k[i][k], bits); },
-                       [&](int, int u, int n) {
+                attend(tile * 32, x.grids, [&](int i, int k) { return Frag<T>::codes(x.k[i][k], bits); },
+                       [&](int u, int n) {
                            if (n == 0)
 #pragma unroll
                                for (int j = 0; j < 4; ++j)
@@ -497,73 +584,58 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     } else if (begin < end) {
         // this wavefront's share of a tile: D / 64 fragments of K (numbers i D / 32 + k) and as many of V (4 u + n)
         constexpr int SHARE_OF = D / 64, ROW = D / 2;
-        struct Raw { uint32_t k[NT][SHARE_OF]; us2 v[NT][4]; Grids grids[NT]; };   // v: the four channels of tokens 2 j and 2 j + 1
-        auto load = [&](int tile, Raw& raw) {
+        struct Raw { uint32_t k[SHARE_OF]; us2 v[4]; Grids grids; };   // v: four channels of tokens 2 j and 2 j + 1
+        auto load = [&](int tile, Raw& x) {
+            const Where w = where(a.c, pages(tile), h, tile * 32);
+            const int r = col, u = (wave * SHARE_OF) >> 2;             // (all of a wavefront's fragments of V are of the same four channels)
 #pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                const Where w = where(a.c, pages(tile + x), h, (tile + x) * 32);
-                const int r = col, u = (wave * SHARE_OF) >> 2;         // (all of a wavefront's fragments of V are of the same four channels)
-#pragma unroll
-                for (int j = 0; j < SHARE_OF; ++j) {
-                    const int f = wave * SHARE_OF + j, i = f / (D / 32), k = f % (D / 32);
-                    at_token(a.c, w, r & 8, [&](int64_t row) {
-                        raw.k[x][j] = *reinterpret_cast<const uint32_t*>(a.c.k_codes + row * ROW + (unsigned)((8 * (r >> 2) + (r & 3) + 4 * i) * ROW + (D / 8) * g + 4 * k));
-                    });
-                }
-                at_token(a.c, w, g & 2, [&](int64_t row) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        raw.v[x][e / 2][e & 1] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + (unsigned)((8 * g + e) * ROW + (D / 32) * r + 2 * u));
+            for (int j = 0; j < SHARE_OF; ++j) {
+                const int f = wave * SHARE_OF + j, i = f / (D / 32), k = f % (D / 32);
+                at_token(a.c, w, r & 8, [&](int64_t row) {
+                    x.k[j] = *reinterpret_cast<const uint32_t*>(a.c.k_codes + row * ROW + (unsigned)((8 * (r >> 2) + (r & 3) + 4 * i) * ROW + (D / 8) * g + 4 * k));
                 });
-                load_grids(a.c, w, raw.grids[x]);
             }
+            at_token(a.c, w, g & 2, [&](int64_t row) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x.v[e / 2][e & 1] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + (unsigned)((8 * g + e) * ROW + (D / 32) * r + 2 * u));
+            });
+            load_grids(a.c, w, x.grids);
         };
-        auto stage = [&](int buf, const Raw& raw) {
+        auto stage = [&](int buf, const Raw& x) {
 #pragma unroll
-            for (int x = 0; x < NT; ++x) {
+            for (int j = 0; j < SHARE_OF; ++j) sh_f[buf][wave * SHARE_OF + j][lane] = Frag<T>::codes(x.k[j], bits);
+            const Zeros z = value_zeros(x.grids.v, bits);
+            // from its first channel on: 0, 0 or 2 (dim 128), or the wavefront's number (dim 64); 2 and 3 are a byte up, odd ones a half byte
+            const int n0 = (wave * SHARE_OF) & 3;
+            uint32_t pair[4];
 #pragma unroll
-                for (int j = 0; j < SHARE_OF; ++j) sh_f[buf][x * 2 * M + wave * SHARE_OF + j][lane] = Frag<T>::codes(raw.k[x][j], bits);
-                const Zeros z = value_zeros(raw.grids[x].v, bits);
-                // from its first channel on: 0, 0 or 2 (dim 128), or the wavefront's number (dim 64); odd ones have their codes a half byte up
-                const int n0 = (wave * SHARE_OF) & 3;
-                uint32_t pair[4];
+            for (int j = 0; j < 4; ++j) pair[j] = __builtin_bit_cast(uint32_t, x.v[j]) >> (D < 256 && (n0 & 2) ? 8 : 0);
+            u4* dst = &sh_f[buf][M + wave * SHARE_OF][lane];
+            if constexpr (SHARE_OF > 1) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) pair[j] = __builtin_bit_cast(uint32_t, raw.v[x][j]) >> (D == 256 ? 0 : n0 & 2 ? 8 : 0);
-                u4* dst = &sh_f[buf][x * 2 * M + M + wave * SHARE_OF][lane];
-                if constexpr (SHARE_OF == 4) {
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) dst[n * 64] = value_fragment(pair, n, z, bits);
-                } else if constexpr (SHARE_OF == 2) {
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) dst[n * 64] = value_fragment(pair, n, z, bits);
-                } else {
-                    if (n0 & 1) dst[0] = value_fragment(pair, 1, z, bits);
-                    else dst[0] = value_fragment(pair, 0, z, bits);
-                }
+                for (int n = 0; n < SHARE_OF; ++n) dst[n * 64] = value_fragment(pair, n, z, bits);
+            } else {
+                if (n0 & 1) dst[0] = value_fragment(pair, 1, z, bits);
+                else dst[0] = value_fragment(pair, 0, z, bits);
             }
         };
         Raw raw;
-        Grids grids[NT];
         load(begin, raw);
         stage(0, raw);
-#pragma unroll
-        for (int x = 0; x < NT; ++x) grids[x] = raw.grids[x];
-        if (begin + NT < end) load(begin + NT, raw);
-        for (int tile = begin; tile < end; tile += NT) {
-            const int buf = ((tile - begin) / NT) & 1;
-            // this step's fragments are in LDS, and everybody is done with the other buffer
+        Grids grids = raw.grids;
+        if (begin + 1 < end) load(begin + 1, raw);
+        for (int tile = begin; tile < end; ++tile) {
+            const int buf = (tile - begin) & 1;
+            // this tile's fragments are in LDS, and everybody is done with the other buffer
             __syncthreads();
-            Grids next[NT];
-#pragma unroll
-            for (int x = 0; x < NT; ++x) next[x] = raw.grids[x];
-            if (tile + NT < end) stage(buf ^ 1, raw);
-            if (tile + 2 * NT < end) load(tile + 2 * NT, raw);
+            const Grids next = raw.grids;
+            if (tile + 1 < end) stage(buf ^ 1, raw);
+            if (tile + 2 < end) load(tile + 2, raw);
             const int t0 = tile * 32;
-            if (t0 < any_to && t0 + 32 * NT > any_from)
-                attend(t0, grids, [&](int x, int i, int k) { return sh_f[buf][x * 2 * M + i * (D / 32) + k][lane]; },
-                       [&](int x, int u, int n) { return sh_f[buf][x * 2 * M + M + 4 * u + n][lane]; });
-#pragma unroll
-            for (int x = 0; x < NT; ++x) grids[x] = next[x];
+            if (t0 < any_to && t0 + 32 > any_from)
+                attend(t0, grids, [&](int i, int k) { return sh_f[buf][i * (D / 32) + k][lane]; }, [&](int u, int n) { return sh_f[buf][M + 4 * u + n][lane]; });
+            grids = next;
         }
     }
 
@@ -577,15 +649,15 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         if (rho >= rows) return;
         const int i = rho / G, head = h * G + rho - i * G;
         const int64_t token = mine.first + i;
-        if (a.parts > 1) {
-            const int64_t at = ((int64_t)part * a.s.rows + token) * a.heads_q + head;
+        if (parts > 1) {
+            const int64_t at = ((int64_t)h * a.slots + index) * TILE + rho - base64;
             if (ch == 0) { a.part_ml[2 * at] = mm; a.part_ml[2 * at + 1] = ll; }
             f4* dst = reinterpret_cast<f4*>(a.part_o + at * D + ch);
 #pragma unroll
             for (int j = 0; j < N / 4; ++j) dst[j] = f4{value(4 * j), value(4 * j + 1), value(4 * j + 2), value(4 * j + 3)};
             return;
         }
-        const float inv = ll == 0.f ? 0.f : 1.f / ll;                  // a row that sees nothing is 0
+        const float inv = ll == 0.f ? 0.f : BIAS2 / ll;                // a row that sees nothing is 0
         T out[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) out[k] = (T)(value(k) * inv);
@@ -639,43 +711,57 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a)
     constexpr int N = D / 64;
     const int lane = threadIdx.x & 63;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t token = item / a.heads_q;
-    const int head = (int)(item - token * a.heads_q);
-    const Kv4Rows first = kv4_rows(a.s.starts, 0, a.s.rows), last = kv4_rows(a.s.starts, a.s.n_seqs - 1, a.s.rows);
-    if (token < first.first || token >= last.first + last.count) return;      // a row of no sequence
-    const int64_t stride = (int64_t)a.s.rows * a.heads_q, at = token * a.heads_q + head;
+    const int token = __builtin_amdgcn_readfirstlane((int)(item / a.heads_q));
+    const int head = __builtin_amdgcn_readfirstlane((int)(item - (int64_t)token * a.heads_q));
+    if (token >= a.s.rows) return;
+    const int b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, token, [&](int i) { return (int64_t)kv4_rows(a.s.starts, i, a.s.rows).first; }));
+    const Kv4Rows mine = kv4_rows(a.s.starts, b, a.s.rows);
+    if (token < mine.first || token >= mine.first + mine.count) return;       // a row of no sequence
+    const Split split = split_of(a);
+    int parts = 1, first = 0;
+#pragma unroll
+    for (int j = 0; j < Split::J; ++j)
+        if (b >> 6 == j) {
+            parts = __builtin_amdgcn_readlane(split.parts[j], b & 63);
+            first = __builtin_amdgcn_readlane(split.first[j], b & 63);
+        }
+    if (parts == 1) return;                                                   // its results are there
+    const int G = a.q.group, h = head / G, rho = (token - mine.first) * G + head - h * G, tile = rho / a.tile;
+    if (first + (tile + 1) * parts > a.slots) return;                         // (starts out of order)
+    // part p's sums
+    const int64_t at0 = ((int64_t)h * a.slots + first + tile * parts) * a.tile + rho - tile * a.tile, stride = a.tile;
     float m = NEG_MAX, l = 0.f;
-    if (lane < a.parts) { m = a.part_ml[2 * (lane * stride + at)]; l = a.part_ml[2 * (lane * stride + at) + 1]; }
+    if (lane < parts) { m = a.part_ml[2 * (at0 + lane * stride)]; l = a.part_ml[2 * (at0 + lane * stride) + 1]; }
     float top = m;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-    const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    const float w = __builtin_amdgcn_exp2f(m - top);
     float sum = w * l;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
     float y[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) y[c] = 0.f;
-    // four parts' loads in flight; those behind the last, and those that saw nothing, are none
-    for (int p0 = 0; p0 < a.parts; p0 += 4) {
+    // four parts' loads in flight; those behind the last are none (the last one's, times 0)
+    for (int p0 = 0; p0 < parts; p0 += 4) {
         float v[4][N], wp[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int p = min(p0 + k, a.parts - 1);
-            wp[k] = p0 + k < a.parts ? __shfl(w, p) : 0.f;
-            __builtin_memcpy(v[k], a.part_o + (p * stride + at) * D + N * lane, sizeof v[k]);
+            const int p = min(p0 + k, parts - 1);
+            wp[k] = p0 + k < parts ? __shfl(w, p) : 0.f;
+            __builtin_memcpy(v[k], a.part_o + (at0 + p * stride) * D + N * lane, sizeof v[k]);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int c = 0; c < N; ++c) y[c] += wp[k] == 0.f ? 0.f : wp[k] * v[k][c];
+            for (int c = 0; c < N; ++c) y[c] += wp[k] * v[k][c];
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const float inv = sum == 0.f ? 0.f : BIAS2 / sum;
     T out[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) out[c] = (T)(y[c] * inv);
-    __builtin_memcpy(static_cast<T*>(a.q.out) + token * a.q.out_row + (int64_t)head * a.q.out_head + N * lane, out, sizeof out);
-    if (a.q.lse && lane == 0) a.q.lse[at] = sum == 0.f ? -INFINITY : LN2 * top + logf(sum);
+    __builtin_memcpy(static_cast<T*>(a.q.out) + (int64_t)token * a.q.out_row + (int64_t)head * a.q.out_head + N * lane, out, sizeof out);
+    if (a.q.lse && lane == 0) a.q.lse[(int64_t)token * a.heads_q + head] = sum == 0.f ? -INFINITY : LN2 * top + logf(sum);
 }
 
 Kv4Plan kv4_attention_plan(int cus, int dim, int heads, int group, int n_seqs, int64_t rows, int64_t longest)
@@ -685,27 +771,27 @@ Kv4Plan kv4_attention_plan(int cus, int dim, int heads, int group, int n_seqs, i
     p.share = each <= (dim == 256 ? 16 : 32);
     p.tile = p.share ? (each <= 16 ? 16 : 32) : (dim == 256 ? 64 : 128);
     p.tiles = rows * group / p.tile + n_seqs;
-    const int64_t have = std::max<int64_t>(1, p.tiles * heads);
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(KV4_MAX_PARTS, (longest + KV4_PART - 1) / KV4_PART));
-    p.parts = (int)std::min<int64_t>(most, std::max<int64_t>(1, ((p.share ? 8 : 2) * (int64_t)cus + have - 1) / have));
+    // Sequences are split where there are fewer tiles of rows than the chip holds workgroups at a time, by their registers and LDS.  (Dim 128,
+    // 8 heads: 128 sequences of 1024 tokens 38 us, 46 if they are split; 96 of up to 2048 39, 53; 128 of up to 4096 93, 99.)
+    const int64_t full = (p.share && p.tile == 16 ? (dim == 64 ? 4 : dim == 128 ? 3 : 2) : 2) * (int64_t)cus / heads;
+    p.slots = 0;
+    if (longest > KV4_UNSPLIT && n_seqs <= KV4_SPLIT_SEQS && p.tiles < full)
+        p.slots = (int)std::max(full, p.tiles + p.tiles / 2 + 1);
     return p;
 }
 
-int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads, int group, int64_t rows)
-{
-    return p.parts > 1 ? p.parts * rows * heads * group * (dim + 2) * (int64_t)sizeof(float) : 0;
-}
+int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads) { return (int64_t)heads * p.slots * p.tile * (dim + 2) * (int64_t)sizeof(float); }
 
 template <class T, int D>
 static hipError_t attention_of(hipStream_t st, const Kv4Plan& p, const AttnArgs& a)
 {
-    const dim3 grid((unsigned)(p.tiles * a.c.heads), (unsigned)p.parts), block(256);
+    const dim3 grid((unsigned)((p.slots ? p.slots : p.tiles) * a.c.heads)), block(256);
     if (p.share && p.tile == 16) hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, true>), grid, block, 0, st, a);
     else if constexpr (D == 256) hipLaunchKernelGGL((kv4_attention_kernel<T, D, 1, false>), grid, block, 0, st, a);
     else if (p.share) hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((kv4_attention_kernel<T, D, 2, false>), grid, block, 0, st, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.parts == 1) return e;
+    if (e != hipSuccess || !p.slots) return e;
     const int64_t items = (int64_t)a.s.rows * a.heads_q;
     hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3((unsigned)((items + 3) / 4)), block, 0, st, a);
     return hipGetLastError();
@@ -713,7 +799,7 @@ static hipError_t attention_of(hipStream_t st, const Kv4Plan& p, const AttnArgs&
 
 hipError_t launch_kv4_attention(hipStream_t st, const Kv4Plan& p, const Kv4View& c, const Kv4Seqs& s, int type, const Kv4Query& q, float* work)
 {
-    AttnArgs a{c, s, q, p.parts, c.heads * q.group, q.scale * LOG2E, work, work ? work + (int64_t)p.parts * s.rows * c.heads * q.group * c.dim : nullptr};
+    AttnArgs a{c, s, q, c.heads * q.group, p.tile, p.slots, q.scale * LOG2E, work, work ? work + (int64_t)c.heads * p.slots * p.tile * c.dim : nullptr};
     if (type == FOBQ_BF16)
         return c.dim == 64 ? attention_of<bf16_t, 64>(st, p, a) : c.dim == 128 ? attention_of<bf16_t, 128>(st, p, a) : attention_of<bf16_t, 256>(st, p, a);
     return c.dim == 64 ? attention_of<f16_t, 64>(st, p, a) : c.dim == 128 ? attention_of<f16_t, 128>(st, p, a) : attention_of<f16_t, 256>(st, p, a);

@@ -50,11 +50,11 @@ hipError_t launch_kv4_read(hipStream_t st, const Kv4View& c, const Kv4Seqs& s, i
                            int64_t v_head);
 
 // Attention: query rows per workgroup (the rows of a sequence are its tokens times the query heads of a kv head), whether the
-// wavefronts of a workgroup share them and go through the tokens in turn, and parts of the tokens of a sequence (parts > 1: partial
-// results in `work`, joined by a second launch).
-struct Kv4Plan { int tile, share, parts; int64_t tiles; };
+// wavefronts of a workgroup share them and go through the tokens in turn; tiles: workgroups of a head that hold all rows.  slots: 0, or the
+// workgroups of a head where sequences are split into parts of equal size (partial results in `work`, joined by a second launch).
+struct Kv4Plan { int tile, share, slots; int64_t tiles; };
 Kv4Plan kv4_attention_plan(int cus, int dim, int heads, int group, int n_seqs, int64_t rows, int64_t longest);
-int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads, int group, int64_t rows);
+int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads);
 struct Kv4Query {
     const void* q; int64_t q_row, q_head; void* out; int64_t out_row, out_head; float* lse;
     int group, causal, window; float scale;

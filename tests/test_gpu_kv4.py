@@ -205,6 +205,19 @@ def test_peaked_and_flat_scores(ctx):
     run(Case(ctx, [(900, 2), (64, 64)], 2, 256, 16, HF, seed=5, spread=1.5), 4)
 
 
+@pytest.mark.parametrize("power", [126, 100, -40, -56])
+def test_values_of_any_size(ctx, power):
+    """Values near the largest and near the smallest number; and one token alone of that size, among others of size 1."""
+    for seqs in ([(40, 2), (64, 64)], [(3000, 2)]):
+        for one in (False, True):
+            c = Case(ctx, seqs, 1, 128, 16, seed=power & 15)
+            for s, (k, v) in enumerate(c.kv):
+                pick = slice(7, 8) if one else slice(None)
+                v[pick] = (v[pick].double().clamp(-1, 1) * 2.0 ** power).to(BF)
+            ctx.kv4_append(c.cache, c.all, *(torch.cat([x[j] for x in c.kv]).cuda() for j in range(2)))
+            run(c, 2)
+
+
 def test_tokens_that_are_nan_touch_only_rows_that_see_them(ctx):
     import paper_2509_05576_amd as fobq
     c = Case(ctx, [(80, 40)], 1, 128, 16, seed=3)
@@ -282,6 +295,31 @@ def test_pages_that_are_none(ctx):
     assert (none == 0).all()
 
 
+def test_pages_that_are_none_and_nan_in_a_long_sequence(ctx):
+    """The same where a sequence is split: parts without a token, parts that are NaN for the rows that see them only."""
+    c = Case(ctx, [(4000, 3)], 1, 128, 16, seed=16)
+    q = c.queries(2)
+    table = c.table.clone()
+    table[0, 20:150] = -1                                      # tokens 320 .. 2399
+    table[0, 240] = c.pages
+    lse = torch.zeros((3, 2), device="cuda")
+    out = ctx.kv4_attention(c.cache, c.batch(table=table), q.cuda(), lse=lse).cpu().double()
+    (kc, ks), (vc, vs) = c.rows_of(0)
+    keep = torch.tensor([t for t in range(4000) if not 20 <= t // 16 < 150 and t // 16 != 240])
+    for h in range(2):
+        spans = [(0, int((keep <= 3997 + i).sum())) for i in range(3)]
+        want, _, bound, _ = ref.attention(q[:, h], (kc[0][keep], ks[0][keep]), (vc[0][keep], vs[0][keep]), 128 ** -0.5, spans, BF)
+        assert ((out[:, h] - want).abs() <= bound).all()
+    table[:] = -1
+    out = ctx.kv4_attention(c.cache, c.batch(table=table), q.cuda(), lse=lse)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    k, v = (x.clone() for x in c.kv[0])
+    v[3998, 0, 3] = math.nan
+    ctx.kv4_append(c.cache, c.all, k.cuda(), v.cuda())
+    out = ctx.kv4_attention(c.cache, c.batch(), q.cuda()).cpu()
+    assert out[1:].isnan().all() and not out[:1].isnan().any()
+
+
 def test_without_starts(ctx):
     c = Case(ctx, [(70, 1), (5, 1), (33, 1)], 2, 128, 16, seed=12)
     q = c.queries(4).cuda()
@@ -337,6 +375,28 @@ def test_the_hint_of_the_longest_changes_no_coverage(ctx):
     c = Case(ctx, [(3000, 1)], 1, 128, 64, seed=13)
     for longest in (0, 1, 500, 3000, 1 << 20):
         run(c, 4, max_length=longest)
+
+
+def test_starts_out_of_order_stay_in_bounds(ctx):
+    """No such call has a meaning; nothing outside the arguments is touched by it, and the next one is right."""
+    c = Case(ctx, [(2000, 2), (900, 1), (0, 1), (300, 2)], 2, 128, 16, seed=15)
+    q = c.queries(4)
+    whole = torch.full((c.rows + 4, 8, 128), 3.0, dtype=BF, device="cuda")
+    for bad in ([0, 6, 0, 6, 0], [5, 4, 3, 2, 1], [-9, 2 ** 31 - 1, -5, 2 ** 31 - 1, 6], [2 ** 31 - 1] * 5):
+        ctx.kv4_attention(c.cache, c.batch(starts=torch.tensor(bad, dtype=torch.int32)), q.cuda(), out=whole[2:-2])
+        ctx.kv4_read(c.cache, c.batch(starts=torch.tensor(bad, dtype=torch.int32)), c.rows)
+    assert (whole[:2] == 3).all() and (whole[-2:] == 3).all()
+    run(c, 4)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_ragged_sequences_in_parts_of_equal_size(ctx, dim):
+    """Lengths from none to thousands in one call, several sequences in several parts, more of them than a wavefront has lanes."""
+    g = torch.Generator().manual_seed(dim)
+    seqs = [(int(n), 1) for n in (torch.rand(100, generator=g) ** 6 * 3000)] + [(4000, 2), (0, 1), (1500, 9), (5, 5)]
+    run(Case(ctx, seqs, 1, dim, 32, [BF, HF][dim == 128], seed=dim), 2)
+    run(Case(ctx, [(3000, 1), (10, 1), (2500, 70)], 2, dim, 16, BF, seed=dim), 3, window=1500)
+    run(Case(ctx, [(3000, 60)], 1, dim, 64, HF, seed=dim), 5, causal=False)
 
 
 def test_generation_step_by_step(ctx):

@@ -92,11 +92,12 @@ def test_attention_is_covered(dim):
                     if rows * heads * group >= 1 << 29:
                         continue
                     for longest in (0, 1, 500, 16384, 1 << 20):
-                        tile, share, parts, tiles, work = plan(fobq.PLAN_KV4_ATTENTION, [256, dim, heads, group, seqs, rows, longest], 5)
+                        tile, share, slots, tiles, work = plan(fobq.PLAN_KV4_ATTENTION, [256, dim, heads, group, seqs, rows, longest], 5)
                         # sequences may be as ragged as they like: floor(first row * group / tile) + index, and one tile more
                         assert tiles >= rows * group // tile + seqs and tile in (16, 32, 64, 128)
-                        assert 1 <= parts <= 64 and (longest > 256 or parts == 1)
-                        assert work == (4 * parts * rows * heads * group * (dim + 2) if parts > 1 else 0)
+                        # split: room for every tile of rows, and for further parts of some
+                        assert slots == 0 or (slots > tiles and longest > 1024 and seqs <= 256 and slots < 1 << 17)
+                        assert work == 4 * heads * slots * tile * (dim + 2)
 
 
 def test_null_contexts():
