@@ -30,7 +30,6 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 
 constexpr float NEG_MAX = -3.402823466e38f;
 constexpr int VALUE_FLOOR = -60;
@@ -314,6 +313,67 @@ __device__ __forceinline__ void load_tokens(const Kv4View& c, Pages p, int h, in
     load_grids(c, w, x.grids);
 }
 
+// The index-th tile of rows, those that see most tokens first (causal; the workgroups that start last then have least to do): its
+// sequence (-1: there are not so many) and its number there.  A tile's level is how many tiles of tokens the sequence has up to its own; the
+// levels are searched for the one that the index falls into.  (3 prompts of 2048 tokens take
+// 12 % less time than in the order of the sequences, 6 of up to 1000 behind 2000 9 %.)
+struct Ranked { int b, tile; Kv4Rows rows; int length; };
+__device__ __forceinline__ Ranked ranked(const AttnArgs& a, int tile_rows, int index)
+{
+    constexpr int J = KV4_SPLIT_SEQS / 64;
+    const int lane = threadIdx.x & 63;
+    int row[J], count[J], length[J], tiles[J], base[J], top = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int b = 64 * j + lane;
+        row[j] = count[j] = length[j] = tiles[j] = base[j] = 0;
+        if (64 * j < a.s.n_seqs && b < a.s.n_seqs) {
+            const Kv4Rows r = kv4_rows(a.s.starts, b, a.s.rows);
+            row[j] = r.first;
+            count[j] = r.count;
+            length[j] = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
+            tiles[j] = (int)(((int64_t)r.count * a.q.group + tile_rows - 1) / tile_rows);
+            base[j] = (int)min((int64_t)max(0, length[j] - r.count) * a.q.group / tile_rows, (int64_t)(1 << 30) - 1);
+            top = max(top, base[j] + tiles[j]);
+        }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = max(top, __shfl_xor(top, off));
+    // tiles at `level` and above
+    auto above = [&](int level) {
+        int sum = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (64 * j < a.s.n_seqs) sum += min(tiles[j], max(0, base[j] + tiles[j] - level));
+        return __builtin_amdgcn_readlane(sum_to_lane(sum), 63);
+    };
+    int level = 0, over = __builtin_amdgcn_readfirstlane(top), higher = 0;
+    Ranked x{-1, 0, Kv4Rows{0, 0}, 0};
+    if (above(0) <= index) return x;
+    while (over - level > 1) {
+        const int mid = level + (over - level) / 2, n = above(mid);
+        if (n > index) level = mid;
+        else { over = mid; higher = n; }
+    }
+    int left = index - higher;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const bool in = base[j] <= level && level < base[j] + tiles[j];
+        const uint64_t all = __ballot(in);
+        const int place = __builtin_amdgcn_mbcnt_hi((unsigned)(all >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)all, 0));
+        const uint64_t hit = __ballot(in && place == left);
+        if (hit) {
+            const int at = __ffsll((unsigned long long)hit) - 1;
+            x.b = 64 * j + at;
+            x.tile = level - __builtin_amdgcn_readlane(base[j], at);
+            x.rows = Kv4Rows{__builtin_amdgcn_readlane(row[j], at), __builtin_amdgcn_readlane(count[j], at)};
+            x.length = __builtin_amdgcn_readlane(length[j], at);
+        }
+        left -= __popcll(all);
+    }
+    return x;
+}
+
 // What is taken off the values' codes, as fp16 with their offset: 1024 + zero for codes in the low half of a byte, 64 + zero (of
 // (1024 + 16 code) / 16) in the high half; of tokens 2 j and 2 j + 1 of the lane's eight.
 struct Zeros { h2 low[4], high[4]; };
@@ -349,15 +409,19 @@ __device__ __forceinline__ u4 value_fragment(const uint32_t (&pair)[4], int n, c
 // WAVES wavefronts, each with QT x 16 query rows.
 //   SHARE: the same rows for all of them; each takes every WAVES-th tile of tokens into its registers, and their sums meet in LDS at the
 //     end.  For few rows, where the tokens are what costs.
-//   otherwise: rows of its own.  All need the same tokens: each turns a quarter of a tile's codes into fragments in LDS, a tile ahead, and
-//     reads all of them: the codes of 32 tokens take 140 vector instructions, a wavefront's softmax of 16 rows over them 80.
+//   otherwise: rows of its own.  All need the same tokens: each turns a quarter of a stage's codes into fragments in LDS, a stage ahead,
+//     and reads all of them.  A stage is 64 tokens (dim 256: 32, for 64 KiB of LDS), with a barrier each: a wavefront's loads are then 16 bytes of
+//     K and whole pairs of bytes of V, and turning them takes 40 vector instructions for 32 tokens, the softmax of 32 rows 160.  These
+//     bound it: of 2.46 GHz, the vector units issue for 61 % and the matrix units work for 29 % of the time, with two wavefronts a
+//     SIMD (3 prompts of about 2048 tokens behind as many, 32 query heads: 345 us, 750 TFLOP/s; with 32 tokens a stage 389).
 template <class T, int D, int QT, bool SHARE>
 __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
 {
     constexpr int WAVES = 4, M = D / 16, TILE = 16 * QT * (SHARE ? 1 : WAVES);
     __shared__ __attribute__((aligned(16))) float sh_o[SHARE ? WAVES : 1][SHARE ? 16 * QT * (D + 4) : 4];
     __shared__ float sh_ml[SHARE ? WAVES : 1][SHARE ? 16 * QT * 2 : 1];
-    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : 2 * M][SHARE ? 1 : 64];   // fragments of K, then of V
+    constexpr int SUB = D == 256 ? 1 : 2;
+    __shared__ u4 sh_f[SHARE ? 1 : 2][SHARE ? 1 : SUB * 2 * M][SHARE ? 1 : 64];   // per tile of 32 tokens the fragments of K, then of V
 
     const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -384,6 +448,13 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
                 part = i - tile_of_rows * parts;
             }
         }
+        if (b < 0) return;
+    } else if (!SHARE && a.s.n_seqs <= KV4_SPLIT_SEQS) {
+        const Ranked x = ranked(a, TILE, index);
+        b = x.b;
+        mine = x.rows;
+        length = x.length;
+        tile_of_rows = x.tile;
         if (b < 0) return;
     } else {
         // sequence b's tiles begin at floor(first row * G / TILE) + b, which leaves room for every sequence's last, partial tile; with
@@ -438,7 +509,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     // what any of the wavefront's rows sees, and what all of them see (rows that are not there may see what they like)
     const int last = max(base, min(base + 16 * QT, rows) - 1);
     const int to0 = a.q.causal ? before + base / G + 1 : length, to1 = a.q.causal ? before + last / G + 1 : length;
-    const int any_to = base < rows ? max(0, to1) : 0, all_to = to0;
+    int any_to = base < rows ? max(0, to1) : 0, all_to = to0;
     const int any_from = a.q.window > 0 ? max(0, to0 - a.q.window) : 0, all_from = a.q.window > 0 ? max(0, to1 - a.q.window) : 0;
 
     // this part's tokens, in tiles of 32; without SHARE the workgroup's rows, and `needed` those tiles that the wavefront's see
@@ -462,17 +533,12 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         for (int j = 0; j < M; ++j) o[t][j] = f4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // 32 tokens: their scores, weights and share of the sums.  key(i, k), value(u, n): the fragments
-    auto attend = [&](int t0, const Grids& grids, auto key, auto value) {
-        // a lane works on the grids of one token; the eight it needs come from the lanes of its quarter
-        const float ka = __uint_as_float(grids.k & 0xffff0000u) * a.scale2, kz = -(Frag<T>::OFFSET + (float)kv4_zero(grids.k));
-        const float va = __uint_as_float(grids.v & 0xffff0000u) * (1.f / BIAS2), vlog = (float)(max((int)(grids.v >> 23), 127 + VALUE_FLOOR) - 127);
-        float kas[8], vtop = VALUE_FLOOR;
-        f4 s[QT][2];
+    // A lane works on the grids of one token; the eight it needs come from the lanes of its quarter.
+    // The scores of 32 tokens, but for their scales.  key(i, k): the fragments
+    auto scores = [&](uint32_t k_grid, f4 (&s)[QT][2], auto key) {
+        const float kz = -(Frag<T>::OFFSET + (float)kv4_zero(k_grid));
         for8([&](auto e) {
             constexpr int E = decltype(e)::value;
-            kas[E] = from_lane<E>(ka);
-            vtop = fmaxf(vtop, from_lane<E>(vlog));
 #pragma unroll
             for (int t = 0; t < QT; ++t) s[t][E >> 2][E & 3] = from_lane<E>(kz) * qsum[t];
         });
@@ -484,8 +550,15 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
 #pragma unroll
                 for (int t = 0; t < QT; ++t) s[t][i] = Frag<T>::mfma(kf, qf[t][k], s[t][i]);
             }
-        // u: scores above the running maximum, in binary orders
-        float u[QT][8], most = -INFINITY;
+    };
+    // u: scores above the running maximum, in binary orders, which is raised where that is needed.  Returns whether all rows see all tokens.
+    auto above = [&](int t0, const Grids& grids, const f4 (&s)[QT][2], float (&u)[QT][8]) {
+        const float ka = __uint_as_float(grids.k & 0xffff0000u) * a.scale2, vlog = (float)(max((int)(grids.v >> 23), 127 + VALUE_FLOOR) - 127);
+        float kas[8], most = -INFINITY;
+        for8([&](auto e) { kas[decltype(e)::value] = from_lane<decltype(e)::value>(ka); });
+        float vtop = fmaxf(vlog, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(vlog), 0xB1, 0xf, 0xf, true)));      // over the eight
+        vtop = fmaxf(vtop, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(vtop), 0x4E, 0xf, 0xf, true)));
+        vtop = fmaxf(vtop, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(vtop), 0x141, 0xf, 0xf, true)));
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -527,7 +600,11 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
                 for (int j = 0; j < M; ++j) o[t][j] *= f;
             }
         }
-        f16x8 p[QT];
+        return whole;
+    };
+    // the weights times the values' scales, and their sums
+    auto weigh = [&](uint32_t v_grid, const float (&u)[QT][8], f16x8 (&p)[QT]) {
+        const float va = __uint_as_float(v_grid & 0xffff0000u) * (1.f / BIAS2);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             float w[8];
@@ -536,14 +613,17 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
             l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
             for8([&](auto e) { p[t][decltype(e)::value] = (f16_t)(w[decltype(e)::value] * from_lane<decltype(e)::value>(va)); });
         }
-        if (!whole) {
-            // nothing also where the token's values are NaN
+    };
+    // nothing from tokens that are not seen, also where their values are NaN
+    auto forget = [&](const float (&u)[QT][8], f16x8 (&p)[QT]) {
 #pragma unroll
-            for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (u[t][e] == -INFINITY) p[t][e] = (f16_t)0.f;
-        }
+            for (int e = 0; e < 8; ++e)
+                if (u[t][e] == -INFINITY) p[t][e] = (f16_t)0.f;
+    };
+    // value(u, n): the fragments
+    auto add = [&](const f16x8 (&p)[QT], auto value) {
 #pragma unroll
         for (int n = 0; n < M; ++n) {
             const u4 vf = value(n >> 2, n & 3);
@@ -562,14 +642,20 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
             auto use = [&](X& x) {
                 const Zeros z = value_zeros(x.grids.v, bits);
                 uint32_t pair[4];
-                attend(tile * 32, x.grids, [&](int i, int k) { return Frag<T>::codes(x.k[i][k], bits); },
-                       [&](int u, int n) {
-                           if (n == 0)
+                f4 s[QT][2];
+                float u[QT][8];
+                f16x8 p[QT];
+                scores(x.grids.k, s, [&](int i, int k) { return Frag<T>::codes(x.k[i][k], bits); });
+                const bool whole = above(tile * 32, x.grids, s, u);
+                weigh(x.grids.v, u, p);
+                if (!whole) forget(u, p);
+                add(p, [&](int w, int n) {
+                    if (n == 0)
 #pragma unroll
-                               for (int j = 0; j < 4; ++j)
-                                   pair[j] = __builtin_amdgcn_perm(x.v[2 * j + 1][u / 2], x.v[2 * j][u / 2], u & 1 ? 0x07060302u : 0x05040100u);
-                           return value_fragment(pair, n, z, bits);
-                       });
+                        for (int j = 0; j < 4; ++j)
+                            pair[j] = __builtin_amdgcn_perm(x.v[2 * j + 1][w / 2], x.v[2 * j][w / 2], w & 1 ? 0x07060302u : 0x05040100u);
+                    return value_fragment(pair, n, z, bits);
+                });
             };
             load_tokens<D>(a.c, pages(tile), h, tile * 32, x0);
             for (;;) {
@@ -582,60 +668,95 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
             }
         }
     } else if (begin < end) {
-        // this wavefront's share of a tile: D / 64 fragments of K (numbers i D / 32 + k) and as many of V (4 u + n)
-        constexpr int SHARE_OF = D / 64, ROW = D / 2;
-        struct Raw { uint32_t k[SHARE_OF]; us2 v[4]; Grids grids; };   // v: four channels of tokens 2 j and 2 j + 1
-        auto load = [&](int tile, Raw& x) {
-            const Where w = where(a.c, pages(tile), h, tile * 32);
-            const int r = col, u = (wave * SHARE_OF) >> 2;             // (all of a wavefront's fragments of V are of the same four channels)
+        // A stage is SUB tiles of 32 tokens.  4 / SUB wavefronts turn a tile's codes into fragments, each OF of K (numbers i D / 32 + k: one
+        // i, adjacent words of a row) and as many of V (4 u + n: one u).
+        constexpr int PER = WAVES / SUB, OF = M / PER, ROW = D / 2;
+        const int sub = wave / PER, f0 = wave % PER * OF, final = end - 1;
+        // Dim 128 has the registers to take the second tile's scores beside the first one's weights, and to read V's fragments ahead (A prompt
+        // of 8192 tokens, 32 query heads: 671 us, 699 without; dim 64 would lose the third wavefront of a SIMD: 155 us, 133 without, for 4 of 2048).
+        constexpr bool AHEAD = D == 128;
+        // a stage may pass the end of the part
+        any_to = min(any_to, end * 32);
+        all_to = min(all_to, end * 32);
 #pragma unroll
-            for (int j = 0; j < SHARE_OF; ++j) {
-                const int f = wave * SHARE_OF + j, i = f / (D / 32), k = f % (D / 32);
-                at_token(a.c, w, r & 8, [&](int64_t row) {
-                    x.k[j] = *reinterpret_cast<const uint32_t*>(a.c.k_codes + row * ROW + (unsigned)((8 * (r >> 2) + (r & 3) + 4 * i) * ROW + (D / 8) * g + 4 * k));
-                });
+        for (int t = 0; t < QT; ++t) to[t] = min(to[t], end * 32);
+        struct Raw { uint32_t k[OF]; uint32_t v[8]; Grids grids[SUB]; };  // v: four channels of a token (put together only when they are here)
+        auto load = [&](int tile, Raw& x) {
+            Where mine;
+#pragma unroll
+            for (int q = 0; q < SUB; ++q) {
+                const int t = min(tile + q, final);
+                const Where w = where(a.c, pages(t), h, t * 32);
+                load_grids(a.c, w, x.grids[q]);
+                if (q == 0 || q == sub) mine = w;
             }
-            at_token(a.c, w, g & 2, [&](int64_t row) {
+            at_token(a.c, mine, col & 8, [&](int64_t row) {
+                const unsigned at = (8 * (col >> 2) + (col & 3) + 4 * (f0 / (D / 32))) * ROW + (D / 8) * g + 4 * (f0 % (D / 32));
+                __builtin_memcpy(x.k, __builtin_assume_aligned(a.c.k_codes + row * ROW + at, 4 * OF), sizeof x.k);
+            });
+            at_token(a.c, mine, g & 2, [&](int64_t row) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    x.v[e / 2][e & 1] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + (unsigned)((8 * g + e) * ROW + (D / 32) * r + 2 * u));
+                    x.v[e] = *reinterpret_cast<const uint16_t*>(a.c.v_codes + row * ROW + (unsigned)((8 * g + e) * ROW + (D / 32) * col + 2 * (f0 >> 2)));
             });
-            load_grids(a.c, w, x.grids);
         };
         auto stage = [&](int buf, const Raw& x) {
+            u4* dst = &sh_f[buf][sub * 2 * M + f0][lane];
 #pragma unroll
-            for (int j = 0; j < SHARE_OF; ++j) sh_f[buf][wave * SHARE_OF + j][lane] = Frag<T>::codes(x.k[j], bits);
-            const Zeros z = value_zeros(x.grids.v, bits);
-            // from its first channel on: 0, 0 or 2 (dim 128), or the wavefront's number (dim 64); 2 and 3 are a byte up, odd ones a half byte
-            const int n0 = (wave * SHARE_OF) & 3;
+            for (int j = 0; j < OF; ++j) dst[j * 64] = Frag<T>::codes(x.k[j], bits);
+            uint32_t grid = x.grids[0].v;
+#pragma unroll
+            for (int q = 1; q < SUB; ++q) grid = q == sub ? x.grids[q].v : grid;
+            const Zeros z = value_zeros(grid, bits);
+            // from channel 0 or (dim 64) 0 or 2 of the four on; 2 and 3 are a byte up
             uint32_t pair[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) pair[j] = __builtin_bit_cast(uint32_t, x.v[j]) >> (D < 256 && (n0 & 2) ? 8 : 0);
-            u4* dst = &sh_f[buf][M + wave * SHARE_OF][lane];
-            if constexpr (SHARE_OF > 1) {
+            for (int j = 0; j < 4; ++j) pair[j] = (x.v[2 * j] | x.v[2 * j + 1] << 16) >> (OF < 4 && (f0 & 2) ? 8 : 0);
 #pragma unroll
-                for (int n = 0; n < SHARE_OF; ++n) dst[n * 64] = value_fragment(pair, n, z, bits);
-            } else {
-                if (n0 & 1) dst[0] = value_fragment(pair, 1, z, bits);
-                else dst[0] = value_fragment(pair, 0, z, bits);
-            }
+            for (int n = 0; n < OF; ++n) dst[(M + n) * 64] = value_fragment(pair, n, z, bits);
         };
         Raw raw;
         load(begin, raw);
         stage(0, raw);
-        Grids grids = raw.grids;
-        if (begin + 1 < end) load(begin + 1, raw);
-        for (int tile = begin; tile < end; ++tile) {
-            const int buf = (tile - begin) & 1;
-            // this tile's fragments are in LDS, and everybody is done with the other buffer
+        Grids grids[SUB];
+#pragma unroll
+        for (int q = 0; q < SUB; ++q) grids[q] = raw.grids[q];
+        if (begin + SUB < end) load(begin + SUB, raw);
+        for (int tile = begin; tile < end; tile += SUB) {
+            const int buf = (tile - begin) / SUB & 1;
+            // this stage's fragments are in LDS, and everybody is done with the other buffer
             __syncthreads();
-            const Grids next = raw.grids;
-            if (tile + 1 < end) stage(buf ^ 1, raw);
-            if (tile + 2 < end) load(tile + 2, raw);
-            const int t0 = tile * 32;
-            if (t0 < any_to && t0 + 32 > any_from)
-                attend(t0, grids, [&](int i, int k) { return sh_f[buf][i * (D / 32) + k][lane]; }, [&](int u, int n) { return sh_f[buf][M + 4 * u + n][lane]; });
-            grids = next;
+            Grids next[SUB];
+#pragma unroll
+            for (int q = 0; q < SUB; ++q) next[q] = raw.grids[q];
+            if (tile + SUB < end) stage(buf ^ 1, raw);
+            if (tile + 2 * SUB < end) load(tile + 2 * SUB, raw);
+            if (tile * 32 < any_to && (tile + SUB) * 32 > any_from) {
+                auto key = [&](int q) { return [&, q](int i, int k) { return sh_f[buf][q * 2 * M + i * (D / 32) + k][lane]; }; };
+                f4 s[AHEAD ? SUB : 1][QT][2];
+                if (AHEAD) scores(grids[0].k, s[0], key(0));
+#pragma unroll
+                for (int q = 0; q < SUB; ++q) {
+                    const int t0 = (tile + q) * 32;
+                    if (!AHEAD && (t0 >= any_to || t0 + 32 <= any_from)) continue;
+                    float u[QT][8];
+                    f16x8 p[QT];
+                    u4 vf[AHEAD ? M : 1];
+                    if (!AHEAD) scores(grids[q].k, s[0], key(q));
+                    const bool whole = above(t0, grids[q], s[AHEAD ? q : 0], u);
+                    if (AHEAD && q + 1 < SUB) scores(grids[SUB - 1].k, s[SUB - 1], key(SUB - 1));
+                    if (AHEAD) {
+#pragma unroll
+                        for (int n = 0; n < M; ++n) vf[n] = sh_f[buf][q * 2 * M + M + n][lane];
+                        __builtin_amdgcn_sched_barrier(0x47E);         // (not to be read where they are used)
+                    }
+                    weigh(grids[q].v, u, p);
+                    if (!whole) forget(u, p);
+                    add(p, [&](int w, int n) { return AHEAD ? vf[AHEAD ? 4 * w + n : 0] : sh_f[buf][q * 2 * M + M + 4 * w + n][lane]; });
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < SUB; ++q) grids[q] = next[q];
         }
     }
 
