@@ -3,8 +3,9 @@
 
 namespace fobq {
 
-constexpr int64_t MAX_SIDE = (int64_t)1 << 29;      // rows and columns of a matrix, packed rows: products with 4 stay in 32 bits
-
+constexpr int64_t MAX_SIDE = (int64_t)1 << 29;      // rows and columns of a matrix, rows times query heads: products with 4 stay in 32 bits
+// A launch has fewer than 2^32 threads: a wavefront for each row of the cache, or for 512 columns of a matrix's row; 256 for a tile.
+constexpr int64_t MAX_ROWS = ((int64_t)1 << 26) - 4, MAX_TILES = ((int64_t)1 << 24) - 1;
 constexpr int64_t MAX_APART = (int64_t)1 << 24;     // rows of a product's matrices: 256 of them stay within 32-bit offsets
 
 static int enter(fobq_ctx* ctx, const DeviceGuard& g) { return g.ok ? FOBQ_OK : set_err(ctx, FOBQ_EHIP, "cannot select device %d", ctx->device); }
@@ -19,6 +20,8 @@ static int check_matrix(fobq_ctx* ctx, const fobq_fp8_matrix* m, const char* nam
     if (!m) return set_err(ctx, FOBQ_EINVAL, "%s is NULL", name);
     if (m->rows < 0 || m->rows >= MAX_SIDE || m->cols < 0 || m->cols >= MAX_SIDE)
         return set_err(ctx, FOBQ_EINVAL, "%s: rows and cols must be in 0..%lld", name, (long long)MAX_SIDE - 1);
+    if (m->rows * ((m->cols + 511) / 512) > MAX_ROWS)
+        return set_err(ctx, FOBQ_EINVAL, "%s: rows times 512 columns must be no more than %lld (got %lld x %lld)", name, (long long)MAX_ROWS, (long long)m->rows, (long long)m->cols);
     if (m->format != FOBQ_E4M3 && m->format != FOBQ_E5M2) return set_err(ctx, FOBQ_EINVAL, "%s: unknown format %d", name, m->format);
     if (m->rows_per_scale != 1 && m->rows_per_scale != 128)
         return set_err(ctx, FOBQ_EINVAL, "%s: rows_per_scale must be 1 or 128 (got %d)", name, m->rows_per_scale);
@@ -47,7 +50,7 @@ static int check_kv4(fobq_ctx* ctx, const fobq_kv4_cache* c, const fobq_kv4_batc
     if (!c->k_codes || !c->v_codes || !c->k_grids || !c->v_grids) return set_err(ctx, FOBQ_EINVAL, "a part of the cache is NULL");
     if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_grids, 16) || !aligned(c->v_grids, 16))
         return set_err(ctx, FOBQ_EINVAL, "the parts of the cache must be 16-byte aligned");
-    if (b->rows < 0 || b->rows >= MAX_SIDE) return set_err(ctx, FOBQ_EINVAL, "rows must be in 0..%lld (got %lld)", (long long)MAX_SIDE - 1, (long long)b->rows);
+    if (b->rows < 0 || b->rows > MAX_ROWS) return set_err(ctx, FOBQ_EINVAL, "rows must be in 0..%lld (got %lld)", (long long)MAX_ROWS, (long long)b->rows);
     if (b->n_seqs < 0 || b->n_seqs > (1 << 20)) return set_err(ctx, FOBQ_EINVAL, "n_seqs must be in 0..2^20 (got %d)", b->n_seqs);
     int shift = 4;
     while ((1 << shift) < c->page_size) ++shift;
@@ -76,6 +79,8 @@ static int check_attention(fobq_ctx* ctx, const fobq_kv4_cache* c, const fobq_kv
     int64_t longest = q->max_length > 0 && q->max_length < holds ? q->max_length : holds;
     if (q->window > 0) longest = longest < q->window ? longest : q->window;
     *p = kv4_attention_plan(ctx->cus, cv->dim, cv->heads, q->group, sv->n_seqs, sv->rows, longest);
+    if (p->tiles * cv->heads > MAX_TILES)
+        return set_err(ctx, FOBQ_EINVAL, "rows * query heads / %d + n_seqs * heads must be no more than %lld", p->tile, (long long)MAX_TILES);
     return FOBQ_OK;
 }
 
@@ -196,6 +201,8 @@ int fobq_fp8_matmul(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8_matr
         return set_err(ctx, FOBQ_EINVAL, "rows must be less than %lld bytes apart", (long long)MAX_APART);
     if (!is_float(type)) return set_err(ctx, FOBQ_EINVAL, "unknown type %d", type);
     if (ld < b.rows) return set_err(ctx, FOBQ_EINVAL, "ld (%lld) is less than the rows of B", (long long)ld);
+    if (((int64_t)a.rows + 63) / 64 * (((int64_t)b.rows + 63) / 64) > MAX_TILES)
+        return set_err(ctx, FOBQ_EINVAL, "Y has more than %lld tiles of 64 x 64", (long long)MAX_TILES);
     if (a.rows == 0 || b.rows == 0) return FOBQ_OK;
     if (!Y || !aligned(Y, float_size(type))) return set_err(ctx, FOBQ_EINVAL, "Y is NULL or not aligned to its elements");
     const Fp8Plan p = fp8_matmul_plan(ctx->cus, a.rows, b.rows, a.cols, type, b.per);

@@ -4,7 +4,8 @@
 // A block's scale is its largest magnitude over the type's largest value (e4m3 448, e5m2 57344), at least 2^-126 (which a block of
 // zeros has); the values are the nearest ones to x / scale, ties to even.  A block that holds an Inf or NaN is NaN throughout.
 // The quotient: with top = 0.875 * 2^9 or * 2^16, x / (most / top) = (0.875 x) / (most / 2^9 or 2^16); one multiplication by the reciprocal
-// and one correction from the remainder round it as a division would, so that a quotient on the border of two 8-bit values is seen as one.  It
+// and one correction from the remainder round it to fp32 as a division would.  Where that lies on the border of two 8-bit values (one of 2^20
+// fp32 quotients, and zeros) the remainder says on which side the quotient lies, so that it is rounded to 8 bits once and not twice.  It
 // never passes the largest value by more than a rounding, which the conversion takes back.
 #include "lowbit.h"
 
@@ -47,6 +48,15 @@ __device__ __forceinline__ float fp8_quotient(const Fp8Scale& s, float x)
     const float y = x * s.pre * s.inv, p = y * s.most, e = fmaf(y, s.most, -p);
     return fmaf(fmaf(x, s.pre, -p) - e, s.corr, y);
 }
+// A quotient y that lies on a border, or not: one step to the side on which x / scale lies if that is not y itself.  (The remainder's sign is
+// exact; an odd fp32 number is on no border.)
+__device__ __forceinline__ float fp8_side(const Fp8Scale& s, float x, float y)
+{
+    const float p = y * s.most, rest = fmaf(x, s.pre, -p) - fmaf(y, s.most, -p);
+    const uint32_t bits = __float_as_uint(y);
+    if (s.most == 0.f || rest == 0.f || (bits & 1)) return y;          // (most 0: y is exact, or NaN)
+    return __uint_as_float(bits + ((rest > 0.f) == (y > 0.f) ? 1 : -1));
+}
 
 // 8 values into 8 bytes of a row, or those of them that the row has
 template <int FORMAT>
@@ -55,6 +65,14 @@ __device__ __forceinline__ void put8(uint8_t* __restrict__ dst, int left, const 
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = fp8_quotient(s, x[i]);
+    // a border has no lower bits than 2^-4 (e5m2: 2^-3) of its value's highest
+    uint32_t low = ~0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) low = min(low, __float_as_uint(y[i]) << 13);
+    if (low == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = fp8_side(s, x[i], y[i]);
+    }
     const uint32_t w[2] = {to_fp8x4<FORMAT>(y[0], y[1], y[2], y[3]), to_fp8x4<FORMAT>(y[4], y[5], y[6], y[7])};
     if (left >= 8) {
         __builtin_memcpy(dst, w, 8);
@@ -116,8 +134,9 @@ template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void fp8_tiles_kernel(const T* __restrict__ x, int64_t ld, Fp8View out)
 {
     const int tid = threadIdx.x, lane = tid & 63;
-    const int col = blockIdx.x * 128 + 8 * (tid & 15), left = out.cols - col;
-    const int64_t row0 = (int64_t)blockIdx.y * 128 + (tid >> 4);
+    const unsigned across = (out.cols + 127) / 128, down = blockIdx.x / across, over = blockIdx.x - down * across;
+    const int col = over * 128 + 8 * (tid & 15), left = out.cols - col;
+    const int64_t row0 = (int64_t)down * 128 + (tid >> 4);
     __shared__ uint32_t part[4];
     float v[8][8];
     uint32_t most = 0;
@@ -139,7 +158,7 @@ __global__ __launch_bounds__(256) void fp8_tiles_kernel(const T* __restrict__ x,
         const int64_t row = row0 + 16 * k;
         if (row < out.rows) put8<FORMAT>(out.values + row * out.ld + col, left, s, v[k]);
     }
-    if (tid == 0) out.scales[(int64_t)blockIdx.x * out.ld_scales + blockIdx.y] = s.scale;
+    if (tid == 0) out.scales[(int64_t)over * out.ld_scales + down] = s.scale;
 }
 
 // The codes of a layer (Section 3: q = scale (code - zero)): code - zero is an integer of at most 15 in magnitude for codes of up to
@@ -183,7 +202,7 @@ static hipError_t quantize_of(hipStream_t s, const void* x, int64_t ld, const Fp
         const int64_t items = (int64_t)out.rows * ((blocks + 3) / 4);
         hipLaunchKernelGGL((fp8_rows_kernel<T, FORMAT>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, static_cast<const T*>(x), ld, out);
     } else {
-        hipLaunchKernelGGL((fp8_tiles_kernel<T, FORMAT>), dim3((unsigned)blocks, (unsigned)((out.rows + 127) / 128)), dim3(256), 0, s, static_cast<const T*>(x), ld, out);
+        hipLaunchKernelGGL((fp8_tiles_kernel<T, FORMAT>), dim3((unsigned)((int64_t)blocks * ((out.rows + 127) / 128))), dim3(256), 0, s, static_cast<const T*>(x), ld, out);
     }
     return hipGetLastError();
 }

@@ -71,6 +71,32 @@ def test_quantize_extremes(ctx, fmt, per):
     assert got.nan_to_num(0.0).abs().max() <= ref.TOP[fmt]
 
 
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("per", [1, 128])
+def test_quotients_beside_a_border(ctx, fmt, per):
+    """Values whose quotients lie on the border of two 8-bit ones, or by it, closer than fp32 tells apart: the side is the exact
+    quotient's (x * top against border * largest, both exact in 64 bits), ties to the even one."""
+    top, keep = (448.0, 3) if fmt == E4 else (57344.0, 2)
+    g = torch.Generator().manual_seed(per)
+    most = (torch.rand((1 if per == 128 else 128, 1), generator=g) + 1.0).expand(128, 1).contiguous()
+    steps = torch.randint(0, 2 ** keep, (128, 511), generator=g).double()
+    power = 2.0 ** torch.randint(-9 if fmt == E4 else -16, 8, (128, 511), generator=g).double()
+    low_power = power.clamp(min=2.0 ** -6 if fmt == E4 else 2.0 ** -14)       # below it the values are evenly spaced
+    below = torch.where(power < low_power, steps * low_power / 2 ** keep, (2 ** keep + steps) * low_power / 2 ** keep)
+    above = below + low_power / 2 ** keep
+    border = (below + above) / 2
+    x = (border * most.double() / top).float()
+    x = torch.stack((x, torch.nextafter(x, x * 2), torch.nextafter(x, x * 0)))[torch.randint(0, 3, x.shape, generator=g), torch.arange(128)[:, None], torch.arange(511)]
+    first = torch.arange(511) % 128 == 127                                     # each block's largest value, in its last place
+    x[:, first] = most.expand(-1, int(first.sum()))
+    x = torch.cat((most, x), 1)[:, :512] * torch.where(torch.rand((128, 512), generator=g) < 0.5, -1.0, 1.0)
+    got = ctx.fp8_quantize(x.cuda(), fmt, per).values.cpu().double()
+    q, m = x[:, 1:].double().abs() * top, border * most.double()
+    want = torch.where((q > m) | ((q == m) & (steps % 2 == 1)), above, below) * x[:, 1:].sign()
+    inner = ~first
+    assert torch.equal(got[:, 1:][:, inner], want[:, inner])
+
+
 def test_quantize_strides_and_what_is_behind(ctx):
     import paper_2509_05576_amd as fobq
     wide = _x(70, 301, torch.bfloat16, 5).cuda()

@@ -22,6 +22,7 @@ GOOD = dict(rows=100, cols=300, ld=304, ld_scales=100, per=1, format=0, values=A
     (dict(format=1), True), (dict(ld=320), True), (dict(ld=300), False), (dict(ld=288), False), (dict(ld=306), False), (dict(ld_scales=99), False),
     (dict(rows=129, per=128, ld_scales=1), False), (dict(per=2), False), (dict(per=0), False), (dict(format=2), False), (dict(format=-1), False),
     (dict(rows=-1), False), (dict(cols=-1), False), (dict(rows=1 << 30, ld_scales=1 << 30), False), (dict(cols=1 << 30, ld=1 << 30), False),
+    (dict(rows=(1 << 26) - 4, ld_scales=1 << 26), True), (dict(rows=(1 << 26) - 3, ld_scales=1 << 26), False), (dict(rows=1 << 17, cols=1 << 18, ld=1 << 18, ld_scales=1 << 26), False),
     (dict(values=0), False), (dict(scales=0), False), (dict(values=A + 8), False), (dict(scales=A + 2), False)])
 def test_matrices(change, ok):
     m = {**GOOD, **change}
@@ -37,6 +38,7 @@ CACHE = dict(pages=10, page_size=16, heads=2, head_dim=128, reserved=0, n_seqs=3
     (dict(page_size=8), False), (dict(page_size=48), False), (dict(page_size=8192), False), (dict(page_size=0), False), (dict(heads=0), False),
     (dict(heads=1025), False), (dict(head_dim=96), False), (dict(head_dim=0), False), (dict(reserved=1), False), (dict(n_seqs=-1), False),
     (dict(rows=-1), False), (dict(max_pages=5), False), (dict(max_pages=-1), False), (dict(max_pages=1 << 26, table_ld=1 << 26), False),
+    (dict(rows=(1 << 26) - 4), True), (dict(rows=(1 << 26) - 3), False),
     (dict(kc=0), False), (dict(vc=A + 8), False), (dict(kg=A + 4), False), (dict(vg=0), False), (dict(table=0), False), (dict(lengths=0), False)])
 def test_caches(change, ok):
     c = {**CACHE, **change}
