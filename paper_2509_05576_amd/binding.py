@@ -655,7 +655,7 @@ def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tens
     if lse is not None and (tuple(_need(lse, ctx, _F32, 2, "lse").shape) != (rows, heads_q) or not lse.is_contiguous()):
         raise TypeError(f"lse: need a contiguous {(rows, heads_q)}, got {tuple(lse.shape)}")
     d = FobqKv4Query(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q.stride(0), q.stride(1), out.stride(0), out.stride(1),
-                     max_length, _FLOAT[q.dtype], heads_q // heads, int(causal), window, dim ** -0.5 if scale is None else scale, 0)
+                     max_length, _FLOAT[q.dtype], heads_q // heads, 1 if causal else 0, min(window, (1 << 31) - 1), dim ** -0.5 if scale is None else scale, 0)
     lib, need = load_library(), ctypes.c_int64(0)
     _check(ctx, lib.fobq_kv4_attention_workspace(ctx, ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), ctypes.byref(need)))
     work = _scratch(ctx, need.value, q.device)

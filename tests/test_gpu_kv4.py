@@ -377,6 +377,22 @@ def test_the_hint_of_the_longest_changes_no_coverage(ctx):
         run(c, 4, max_length=longest)
 
 
+@pytest.mark.parametrize("count", [70, 300])
+def test_prompts_of_many_sequences(ctx, count):
+    """Rows of their own for every wavefront, more sequences than a wavefront has lanes, and than are put in order; empty ones between."""
+    g = torch.Generator().manual_seed(count)
+    seqs = [(int(n) + 60, 60) if i % 7 else (i, 0) for i, n in enumerate(torch.randint(0, 90, (count,), generator=g))]
+    run(Case(ctx, seqs, 1, 64, 16, [BF, HF][count == 70], seed=count), 1)
+
+
+def test_a_window_beyond_every_length(ctx):
+    c = Case(ctx, [(100, 3), (40, 40)], 1, 128, 16, seed=17)
+    q = c.queries(2).cuda()
+    want = ctx.kv4_attention(c.cache, c.batch(), q)
+    for window in (101, 1 << 20, (1 << 31) - 1, (1 << 32) + 1):
+        assert torch.equal(ctx.kv4_attention(c.cache, c.batch(), q, window=window), want)
+
+
 def test_starts_out_of_order_stay_in_bounds(ctx):
     """No such call has a meaning; nothing outside the arguments is touched by it, and the next one is right."""
     c = Case(ctx, [(2000, 2), (900, 1), (0, 1), (300, 2)], 2, 128, 16, seed=15)

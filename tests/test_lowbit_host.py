@@ -126,3 +126,13 @@ def test_host_tensors_are_refused():
                  lambda: fobq.fobq_kv4_read(1, cache, batch, 1), lambda: fobq.fobq_kv4_attention(1, cache, batch, rows)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("type", [0, 1, 2])
+def test_scratch_of_a_product_is_the_same_for_both_kinds_of_scales(type):
+    for cus in (64, 256):
+        for m in (1, 17, 64, 200, 1000, 5000):
+            for n in (16, 300, 1000, 4096, 20000):
+                for k in (1, 128, 2304, 9000):
+                    a, b = (plan(fobq.PLAN_FP8_MATMUL, [cus, m, n, k, type, per], 5) for per in (1, 128))
+                    assert a[4] == b[4]
