@@ -50,6 +50,7 @@ struct AttnArgs {
     float scale2;          // scale * log2(e)
     float* part_o;         // heads x slots x tile x dim: sums of the rows of a split sequence's part
     float* part_ml;        // the same without dim: maximum (in binary orders) and sum of the weights
+    int2* seqs;            // per sequence its first workgroup and its parts, for the launch that joins them
 };
 
 // How the sequences are split into parts of about equal size, which the host cannot know: the lengths are on the device.  A sequence has
@@ -414,7 +415,8 @@ __device__ __forceinline__ u4 value_fragment(const uint32_t (&pair)[4], int n, c
 //     and reads all of them.  A stage is 64 tokens (dim 256: 32, for 64 KiB of LDS), with a barrier each: a wavefront's loads are then 16 bytes of
 //     K and whole pairs of bytes of V, and turning them takes 40 vector instructions for 32 tokens, the softmax of 32 rows 160.  These
 //     bound it: of 2.46 GHz, the vector units issue for 61 % and the matrix units work for 29 % of the time, with two wavefronts a
-//     SIMD (3 prompts of about 2048 tokens behind as many, 32 query heads: 345 us, 750 TFLOP/s; with 32 tokens a stage 389).
+//     SIMD (3 prompts of about 2048 tokens behind as many, 32 query heads: 347 us, 745 TFLOP/s; with 32 tokens a stage 389; with eight
+//     wavefronts a workgroup, which turn half as many codes each but keep in step, 406).
 template <class T, int D, int QT, bool SHARE>
 __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
 {
@@ -435,6 +437,9 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     Kv4Rows mine{0, 0};
     if (a.slots) {
         const Split split = split_of(a);
+#pragma unroll
+        for (int j = 0; j < Split::J; ++j)
+            if (blockIdx.x == 0 && wave == 0 && 64 * j + lane < a.s.n_seqs) a.seqs[64 * j + lane] = int2{split.first[j], split.parts[j]};
 #pragma unroll
         for (int j = 0; j < Split::J; ++j) {
             const uint64_t hit = __ballot(index >= split.first[j] && index < split.first[j] + split.items[j]);
@@ -826,8 +831,8 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     }
 }
 
-// The parts of a row joined: one wavefront per row and query head.  Parts whose rows saw nothing have a sum of 0.  (1024 rows: 5 us, most of
-// which is the launch and finding the split again.)
+// The parts of a row joined: one wavefront per row and query head.  Parts whose rows saw nothing have a sum of 0.  (1024 rows: 4 us, most of
+// which is the launch; finding the split again here, instead of reading it, took 2 more.)
 template <class T, int D>
 __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a)
 {
@@ -840,14 +845,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a)
     const int b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, token, [&](int i) { return (int64_t)kv4_rows(a.s.starts, i, a.s.rows).first; }));
     const Kv4Rows mine = kv4_rows(a.s.starts, b, a.s.rows);
     if (token < mine.first || token >= mine.first + mine.count) return;       // a row of no sequence
-    const Split split = split_of(a);
-    int parts = 1, first = 0;
-#pragma unroll
-    for (int j = 0; j < Split::J; ++j)
-        if (b >> 6 == j) {
-            parts = __builtin_amdgcn_readlane(split.parts[j], b & 63);
-            first = __builtin_amdgcn_readlane(split.first[j], b & 63);
-        }
+    const int first = __builtin_amdgcn_readfirstlane(a.seqs[b].x), parts = __builtin_amdgcn_readfirstlane(a.seqs[b].y);
     if (parts == 1) return;                                                   // its results are there
     const int G = a.q.group, h = head / G, rho = (token - mine.first) * G + head - h * G, tile = rho / a.tile;
     if (first + (tile + 1) * parts > a.slots) return;                         // (starts out of order)
@@ -903,7 +901,10 @@ Kv4Plan kv4_attention_plan(int cus, int dim, int heads, int group, int n_seqs, i
     return p;
 }
 
-int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads) { return (int64_t)heads * p.slots * p.tile * (dim + 2) * (int64_t)sizeof(float); }
+int64_t kv4_attention_workspace(const Kv4Plan& p, int dim, int heads)
+{
+    return p.slots ? (int64_t)heads * p.slots * p.tile * (dim + 2) * (int64_t)sizeof(float) + KV4_SPLIT_SEQS * (int64_t)sizeof(int2) : 0;
+}
 
 template <class T, int D>
 static hipError_t attention_of(hipStream_t st, const Kv4Plan& p, const AttnArgs& a)
@@ -922,7 +923,11 @@ static hipError_t attention_of(hipStream_t st, const Kv4Plan& p, const AttnArgs&
 
 hipError_t launch_kv4_attention(hipStream_t st, const Kv4Plan& p, const Kv4View& c, const Kv4Seqs& s, int type, const Kv4Query& q, float* work)
 {
-    AttnArgs a{c, s, q, c.heads * q.group, p.tile, p.slots, q.scale * LOG2E, work, work ? work + (int64_t)c.heads * p.slots * p.tile * c.dim : nullptr};
+    AttnArgs a{c, s, q, c.heads * q.group, p.tile, p.slots, q.scale * LOG2E, work, nullptr, nullptr};
+    if (work) {
+        a.part_ml = work + (int64_t)c.heads * p.slots * p.tile * c.dim;
+        a.seqs = reinterpret_cast<int2*>(a.part_ml + (int64_t)c.heads * p.slots * p.tile * 2);
+    }
     if (type == FOBQ_BF16)
         return c.dim == 64 ? attention_of<bf16_t, 64>(st, p, a) : c.dim == 128 ? attention_of<bf16_t, 128>(st, p, a) : attention_of<bf16_t, 256>(st, p, a);
     return c.dim == 64 ? attention_of<f16_t, 64>(st, p, a) : c.dim == 128 ? attention_of<f16_t, 128>(st, p, a) : attention_of<f16_t, 256>(st, p, a);

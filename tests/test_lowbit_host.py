@@ -99,7 +99,8 @@ def test_attention_is_covered(dim):
                         assert tiles >= rows * group // tile + seqs and tile in (16, 32, 64, 128)
                         # split: room for every tile of rows, and for further parts of some
                         assert slots == 0 or (slots > tiles and longest > 1024 and seqs <= 256 and slots < 1 << 17)
-                        assert work == 4 * heads * slots * tile * (dim + 2)
+                        # sums, maxima and weights of every slot, and where each sequence's slots begin
+                        assert work == (4 * heads * slots * tile * (dim + 2) + 8 * 256 if slots else 0)
 
 
 def test_null_contexts():
@@ -126,13 +127,3 @@ def test_host_tensors_are_refused():
                  lambda: fobq.fobq_kv4_read(1, cache, batch, 1), lambda: fobq.fobq_kv4_attention(1, cache, batch, rows)):
         with pytest.raises(TypeError):
             call()
-
-
-@pytest.mark.parametrize("type", [0, 1, 2])
-def test_scratch_of_a_product_is_the_same_for_both_kinds_of_scales(type):
-    for cus in (64, 256):
-        for m in (1, 17, 64, 200, 1000, 5000):
-            for n in (16, 300, 1000, 4096, 20000):
-                for k in (1, 128, 2304, 9000):
-                    a, b = (plan(fobq.PLAN_FP8_MATMUL, [cus, m, n, k, type, per], 5) for per in (1, 128))
-                    assert a[4] == b[4]
