@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -39,26 +40,12 @@ class FobqOut(ctypes.Structure):
                 ("Hinv_work", ctypes.c_void_p), ("loss", ctypes.c_void_p)]
 
 
-class FobqFp8Matrix(ctypes.Structure):
-    _fields_ = [("values", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
-                ("ld", ctypes.c_int64), ("ld_scales", ctypes.c_int64), ("rows_per_scale", ctypes.c_int32), ("format", ctypes.c_int32)]
-
-
-class FobqKv4Cache(ctypes.Structure):
-    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_grids", ctypes.c_void_p), ("v_grids", ctypes.c_void_p),
-                ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("reserved", ctypes.c_int32)]
-
-
-class FobqKv4Batch(ctypes.Structure):
-    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("rows", ctypes.c_int64),
-                ("table_ld", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
-
-
-class FobqKv4Query(ctypes.Structure):
-    _fields_ = [("Q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_row", ctypes.c_int64), ("q_head", ctypes.c_int64),
-                ("out_row", ctypes.c_int64), ("out_head", ctypes.c_int64), ("max_length", ctypes.c_int64), ("type", ctypes.c_int32),
-                ("group", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+# The structs of the calls that run a quantized network, as bytes with C's layout: fobq_fp8_matrix, fobq_kv4_cache, fobq_kv4_batch, fobq_kv4_query
+# in the order of their fields.  (A ctypes structure takes four times as long to fill, and these calls are short.)
+_fp8_matrix = struct.Struct("@PPqqqqii").pack
+_kv4_cache = struct.Struct("@PPPPqiiii").pack
+_kv4_batch = struct.Struct("@PPPqqii").pack
+_kv4_query = struct.Struct("@PPPqqqqqiiiifi").pack
 
 
 class FobqLayer(ctypes.Structure):
@@ -104,14 +91,14 @@ def load_library() -> ctypes.CDLL:
     lib.fobq_hessian_form.argtypes = [vp, ctypes.POINTER(i32)]
     lib.fobq_obq_rows.argtypes = [vp, vp, i64, i64, vp, ctypes.POINTER(FobqOpts), i64, i64, vp, vp, vp, vp]
     ptr = ctypes.POINTER
-    lib.fobq_fp8_quantize.argtypes = [vp, vp, i32, i64, ptr(FobqFp8Matrix)]
-    lib.fobq_fp8_from_codes.argtypes = [vp, vp, vp, vp, i32, i32, ptr(FobqFp8Matrix)]
-    lib.fobq_fp8_matmul.argtypes = [vp, ptr(FobqFp8Matrix), ptr(FobqFp8Matrix), vp, i32, i64, vp, i64]
+    lib.fobq_fp8_quantize.argtypes = [vp, vp, i32, i64, vp]
+    lib.fobq_fp8_from_codes.argtypes = [vp, vp, vp, vp, i32, i32, vp]
+    lib.fobq_fp8_matmul.argtypes = [vp, vp, vp, vp, i32, i64, vp, i64]
     lib.fobq_fp8_matmul_workspace.argtypes = [vp, i64, i64, i64, i32, ptr(i64)]
-    lib.fobq_kv4_append.argtypes = [vp, ptr(FobqKv4Cache), ptr(FobqKv4Batch), i32, vp, i64, i64, vp, i64, i64]
+    lib.fobq_kv4_append.argtypes = [vp, vp, vp, i32, vp, i64, i64, vp, i64, i64]
     lib.fobq_kv4_read.argtypes = lib.fobq_kv4_append.argtypes
-    lib.fobq_kv4_attention.argtypes = [vp, ptr(FobqKv4Cache), ptr(FobqKv4Batch), ptr(FobqKv4Query), vp, i64]
-    lib.fobq_kv4_attention_workspace.argtypes = [vp, ptr(FobqKv4Cache), ptr(FobqKv4Batch), ptr(FobqKv4Query), ptr(i64)]
+    lib.fobq_kv4_attention.argtypes = [vp, vp, vp, vp, vp, i64]
+    lib.fobq_kv4_attention_workspace.argtypes = [vp, vp, vp, vp, ptr(i64)]
     lib.fobq_probe_int8_matrix_rate.argtypes = [vp, i32, ctypes.POINTER(dbl)]
     lib.fobq_profile_enable.argtypes = [vp, i32]
     lib.fobq_profile_get.argtypes = [vp, i32, ctypes.POINTER(dbl), ctypes.POINTER(i64)]
@@ -433,7 +420,7 @@ _current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda
 
 def _need(t: torch.Tensor, ctx: int, dtypes, dims: int, what: str) -> torch.Tensor:
     """A device tensor of one of these types whose last dimension is adjacent, on the context's device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dim() != dims or (t.stride()[-1] != 1 and t.shape[-1] > 1):
         names = " or ".join(str(d) for d in dtypes)
         got = f"{tuple(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
         raise TypeError(f"{what}: need a {dims}-D device tensor of {names} with adjacent last dimension, got {got}")
@@ -461,17 +448,18 @@ class Fp8Matrix:
     rows_per_scale: int = 1
 
 
-def _fp8(ctx: int, m: Fp8Matrix, what: str) -> FobqFp8Matrix:
+def _fp8(ctx: int, m: Fp8Matrix, what: str):
+    """What the library calls a matrix, its rows and columns."""
     v, s, per = _need(m.values, ctx, _FP8, 2, what + ".values"), _need(m.scales, ctx, _F32, 2, what + ".scales"), m.rows_per_scale
     (rows, cols), (sc, sr) = v.shape, s.shape
     wide = (cols + 15) & -16
     if per not in (1, 128) or sc != (cols + 127) // 128 or sr != (rows + per - 1) // per:
         raise TypeError(f"{what}: rows_per_scale must be 1 or 128 and scales (ceil(cols / 128), ceil(rows / rows_per_scale)), "
                         f"got {per} and {(sc, sr)} for {rows} x {cols}")
-    ld = v.stride(0) if rows > 1 and cols else wide
+    ld = v.stride()[0] if rows > 1 and cols else wide
     if wide != cols and rows and v.storage_offset() + (rows - 1) * ld + wide > v.untyped_storage().nbytes():
         raise TypeError(f"{what}: the last row must be readable to a multiple of 16 bytes")
-    return FobqFp8Matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, s.stride(0) if sc > 1 else sr, per, _FP8[v.dtype])
+    return _fp8_matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, s.stride()[0] if sc > 1 else sr, per, _FP8[v.dtype]), rows, cols
 
 
 def _new_fp8(ctx: int, rows: int, cols: int, format: torch.dtype, per: int, device):
@@ -481,15 +469,15 @@ def _new_fp8(ctx: int, rows: int, cols: int, format: torch.dtype, per: int, devi
     wide, sr = (cols + 15) & -16, (rows + per - 1) // per
     values, scales = _empty(ctx, (rows, wide), format, device), _empty(ctx, ((cols + 127) // 128, sr), torch.float32, device)
     return (Fp8Matrix(values if wide == cols else values[:, :cols], scales, per),
-            FobqFp8Matrix(values.data_ptr(), scales.data_ptr(), rows, cols, wide, sr, per, _FP8[format]))
+            _fp8_matrix(values.data_ptr(), scales.data_ptr(), rows, cols, wide, sr, per, _FP8[format]))
 
 
 def _out_fp8(ctx: int, out: Optional[Fp8Matrix], rows: int, cols: int, format: torch.dtype, per: int, device):
     if out is None:
         return _new_fp8(ctx, rows, cols, format, per, device)
-    m = _fp8(ctx, out, "out")
-    if m.rows != rows or m.cols != cols:
-        raise TypeError(f"out is {m.rows} x {m.cols}, need {rows} x {cols}")
+    m, r, c = _fp8(ctx, out, "out")
+    if r != rows or c != cols:
+        raise TypeError(f"out is {r} x {c}, need {rows} x {cols}")
     return out, m
 
 
@@ -499,7 +487,7 @@ def fobq_fp8_quantize(ctx: int, X: torch.Tensor, format: torch.dtype = torch.flo
     _need(X, ctx, _FLOAT, 2, "X")
     rows, cols = X.shape
     out, m = _out_fp8(ctx, out, rows, cols, format, rows_per_scale, X.device)
-    _check(ctx, load_library().fobq_fp8_quantize(ctx, X.data_ptr(), _FLOAT[X.dtype], X.stride(0) if rows > 1 else cols, ctypes.byref(m)))
+    _check(ctx, load_library().fobq_fp8_quantize(ctx, X.data_ptr(), _FLOAT[X.dtype], X.stride()[0] if rows > 1 else cols, m))
     return out
 
 
@@ -517,7 +505,7 @@ def fobq_fp8_from_codes(ctx: int, codes: torch.Tensor, scales: torch.Tensor, zer
         raise TypeError("codes: need a contiguous tensor")
     out, m = _out_fp8(ctx, out, rows, cols, torch.float8_e4m3fn, 1, codes.device)
     group = cols // scales.shape[1] if scales.shape[1] > 1 else 0
-    _check(ctx, load_library().fobq_fp8_from_codes(ctx, codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), bits, group, ctypes.byref(m)))
+    _check(ctx, load_library().fobq_fp8_from_codes(ctx, codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), bits, group, m))
     return out
 
 
@@ -527,22 +515,23 @@ def _scratch(ctx: int, need: int, device) -> Optional[torch.Tensor]:
 
 def fobq_fp8_matmul(ctx: int, A: Fp8Matrix, B: Fp8Matrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """A (activations, m x k) times B (weights, n x k) transposed -> m x n of `dtype` (fp32, bf16 or fp16), or into `out`."""
-    a, b = _fp8(ctx, A, "A"), _fp8(ctx, B, "B")
-    if a.cols != b.cols:
-        raise TypeError(f"A has {a.cols} columns, B {b.cols}")
+    (a, m, k), (b, n, k2) = _fp8(ctx, A, "A"), _fp8(ctx, B, "B")
+    if k != k2:
+        raise TypeError(f"A has {k} columns, B {k2}")
     device = A.values.device
     if out is None:
         if dtype not in _FLOAT:
             raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        out = _empty(ctx, (a.rows, b.rows), dtype, device)
+        out = _empty(ctx, (m, n), dtype, device)
     else:
         _need(out, ctx, _FLOAT, 2, "out")
-        if tuple(out.shape) != (a.rows, b.rows):
-            raise TypeError(f"out: need {a.rows} x {b.rows}, got {tuple(out.shape)}")
+        if tuple(out.shape) != (m, n):
+            raise TypeError(f"out: need {m} x {n}, got {tuple(out.shape)}")
+        dtype = out.dtype
     lib, need = load_library(), ctypes.c_int64(0)
-    _check(ctx, lib.fobq_fp8_matmul_workspace(ctx, a.rows, b.rows, a.cols, _FLOAT[out.dtype], ctypes.byref(need)))
+    _check(ctx, lib.fobq_fp8_matmul_workspace(ctx, m, n, k, _FLOAT[dtype], ctypes.byref(need)))
     work = _scratch(ctx, need.value, device)
-    _check(ctx, lib.fobq_fp8_matmul(ctx, ctypes.byref(a), ctypes.byref(b), out.data_ptr(), _FLOAT[out.dtype], out.stride(0) if a.rows > 1 else b.rows,
+    _check(ctx, lib.fobq_fp8_matmul(ctx, a, b, out.data_ptr(), _FLOAT[dtype], out.stride()[0] if m > 1 else n,
                                     work.data_ptr() if work is not None else None, need.value))
     return out
 
@@ -572,7 +561,7 @@ class Kv4Batch:
 
 
 def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
-    """What the library calls a cache and a batch."""
+    """What the library calls a cache and a batch, and the cache's heads and channels."""
     k, v, kg, vg, table, lengths, starts = cache.k_codes, cache.v_codes, cache.k_grids, cache.v_grids, batch.table, batch.lengths, batch.starts
     home, u8, i32 = _streams.get(ctx), torch.uint8, torch.int32
     dev = home[0] if home is not None else None
@@ -585,7 +574,7 @@ def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
                 and k.get_device() == dev and v.get_device() == dev and kg.get_device() == dev and vg.get_device() == dev
                 and table.get_device() == dev and lengths.get_device() == dev and v.shape == shape and grid == shape[:3] and vg.shape == grid
                 and k.is_contiguous() and v.is_contiguous() and kg.is_contiguous() and vg.is_contiguous()
-                and (table.stride(1) == 1 or width <= 1) and lengths.shape == (n,) and lengths.is_contiguous()
+                and ((strides := table.stride())[1] == 1 or width <= 1) and lengths.shape == (n,) and lengths.is_contiguous()
                 and (starts is None or (starts.dtype is i32 and starts.get_device() == dev and starts.shape == (n + 1,) and starts.is_contiguous())))
     except (AttributeError, ValueError):
         fine = False
@@ -603,38 +592,38 @@ def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
         if starts is not None and _need(starts, ctx, _I32, 1, "starts").shape[0] != n + 1:
             raise TypeError(f"starts: need {n + 1} entries, got {starts.shape[0]}")
         pages, heads, page, half = k.shape
-        width = table.shape[1]
-    return (FobqKv4Cache(k.data_ptr(), v.data_ptr(), kg.data_ptr(), vg.data_ptr(), pages, page, heads, 2 * half, 0),
-            FobqKv4Batch(table.data_ptr(), lengths.data_ptr(), starts.data_ptr() if starts is not None else None, rows,
-                         table.stride(0) if n > 1 else width, n, width))
+        width, strides = table.shape[1], table.stride()
+    return (_kv4_cache(k.data_ptr(), v.data_ptr(), kg.data_ptr(), vg.data_ptr(), pages, page, heads, 2 * half, 0),
+            _kv4_batch(table.data_ptr(), lengths.data_ptr(), starts.data_ptr() if starts is not None else 0, rows,
+                       strides[0] if n > 1 else width, n, width), heads, 2 * half)
 
 
-def _kv_rows(ctx: int, c: FobqKv4Cache, k: torch.Tensor, v: torch.Tensor, rows: int, dtypes):
+def _kv_rows(ctx: int, heads: int, dim: int, k: torch.Tensor, v: torch.Tensor, rows: int, dtypes):
     shape = _need(k, ctx, dtypes, 3, "k").shape
     _need(v, ctx, dtypes, 3, "v")
-    if v.shape != shape or k.dtype != v.dtype or shape[0] != rows or shape[1] != c.heads or shape[2] != c.head_dim:
-        raise TypeError(f"k and v: need {(rows, c.heads, c.head_dim)} of one type, got {tuple(shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
-    return (_FLOAT[k.dtype], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1))
+    if v.shape != shape or k.dtype != v.dtype or shape != (rows, heads, dim):
+        raise TypeError(f"k and v: need {(rows, heads, dim)} of one type, got {tuple(shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
+    (k_row, k_head, _), (v_row, v_head, _) = k.stride(), v.stride()
+    return (_FLOAT[k.dtype], k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head)
 
 
 def fobq_kv4_append(ctx: int, cache: Kv4Cache, batch: Kv4Batch, k: torch.Tensor, v: torch.Tensor) -> None:
     """New keys and values (bf16 or fp16, rows x heads x head_dim, any row and head strides) into the sequences' last places."""
-    c, b = _kv4(ctx, cache, batch, k.shape[0])
-    args = _kv_rows(ctx, c, k, v, b.rows, _HALF)
-    _check(ctx, load_library().fobq_kv4_append(ctx, ctypes.byref(c), ctypes.byref(b), *args))
+    rows = k.shape[0]
+    c, b, heads, dim = _kv4(ctx, cache, batch, rows)
+    _check(ctx, load_library().fobq_kv4_append(ctx, c, b, *_kv_rows(ctx, heads, dim, k, v, rows, _HALF)))
 
 
 def fobq_kv4_read(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int, dtype: torch.dtype = torch.bfloat16, out=None):
     """What the packed rows' places in the cache stand for: (k, v), rows x heads x head_dim of `dtype`, or into out = (k, v)."""
-    c, b = _kv4(ctx, cache, batch, rows)
+    c, b, heads, dim = _kv4(ctx, cache, batch, rows)
     if out is None:
         if dtype not in _FLOAT:
             raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        shape, device = (rows, c.heads, c.head_dim), cache.k_codes.device
+        shape, device = (rows, heads, dim), cache.k_codes.device
         out = (_empty(ctx, shape, dtype, device), _empty(ctx, shape, dtype, device))
     k, v = out
-    args = _kv_rows(ctx, c, k, v, rows, _FLOAT)
-    _check(ctx, load_library().fobq_kv4_read(ctx, ctypes.byref(c), ctypes.byref(b), *args))
+    _check(ctx, load_library().fobq_kv4_read(ctx, c, b, *_kv_rows(ctx, heads, dim, k, v, rows, _FLOAT)))
     return k, v
 
 
@@ -644,22 +633,22 @@ def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tens
     unless given.  max_length: the most tokens a sequence holds, if known (a hint).  lse (fp32, rows x query heads): filled."""
     _need(q, ctx, _HALF, 3, "q")
     rows, heads_q, dim = q.shape
-    c, b = _kv4(ctx, cache, batch, rows)
-    heads = c.heads
-    if dim != c.head_dim or heads < 1 or heads_q < 1 or heads_q % heads:
-        raise TypeError(f"q: need rows x (a multiple of {heads}) x {c.head_dim}, got {tuple(q.shape)}")
+    c, b, heads, channels = _kv4(ctx, cache, batch, rows)
+    if dim != channels or heads < 1 or heads_q < 1 or heads_q % heads:
+        raise TypeError(f"q: need rows x (a multiple of {heads}) x {channels}, got {tuple(q.shape)}")
     if out is None:
         out = _empty(ctx, (rows, heads_q, dim), q.dtype, q.device)
     elif _need(out, ctx, (q.dtype,), 3, "out").shape != q.shape:
         raise TypeError(f"out: need {tuple(q.shape)}, got {tuple(out.shape)}")
     if lse is not None and (tuple(_need(lse, ctx, _F32, 2, "lse").shape) != (rows, heads_q) or not lse.is_contiguous()):
         raise TypeError(f"lse: need a contiguous {(rows, heads_q)}, got {tuple(lse.shape)}")
-    d = FobqKv4Query(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None, q.stride(0), q.stride(1), out.stride(0), out.stride(1),
-                     max_length, _FLOAT[q.dtype], heads_q // heads, 1 if causal else 0, min(window, (1 << 31) - 1), dim ** -0.5 if scale is None else scale, 0)
+    (q_row, q_head, _), (o_row, o_head, _) = q.stride(), out.stride()
+    d = _kv4_query(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else 0, q_row, q_head, o_row, o_head, max_length, _FLOAT[q.dtype],
+                   heads_q // heads, 1 if causal else 0, min(window, (1 << 31) - 1), dim ** -0.5 if scale is None else scale, 0)
     lib, need = load_library(), ctypes.c_int64(0)
-    _check(ctx, lib.fobq_kv4_attention_workspace(ctx, ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), ctypes.byref(need)))
+    _check(ctx, lib.fobq_kv4_attention_workspace(ctx, c, b, d, ctypes.byref(need)))
     work = _scratch(ctx, need.value, q.device)
-    _check(ctx, lib.fobq_kv4_attention(ctx, ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), work.data_ptr() if work is not None else None, need.value))
+    _check(ctx, lib.fobq_kv4_attention(ctx, c, b, d, work.data_ptr() if work is not None else None, need.value))
     return out
 
 

@@ -1,5 +1,6 @@
 """Plain 64-bit forms of the 8-bit block matrices and of the 4-bit cache with its attention, on the CPU, from their definitions, with
 the bounds that the kernels' arithmetic gives."""
+import ctypes
 import math
 
 import torch
@@ -113,3 +114,16 @@ def attention(q, k, v, scale, spans, dtype):
         bound[i] += HALF[dtype] * out[i].abs() * 1.01 + 1e-37
         lbound[i] = 2 * ds + (n + 64) * U + 4 * U * lse[i].abs()
     return out, lse, bound, lbound
+
+
+# ---- the structs of include/fobq.h, for calls with fields of their own ----------------------------------------------
+def _struct(name, pointers, longs, ints, floats=(), last=()):
+    fields = [(n, ctypes.c_void_p) for n in pointers] + [(n, ctypes.c_int64) for n in longs] + [(n, ctypes.c_int32) for n in ints]
+    return type(name, (ctypes.Structure,), {"_fields_": fields + [(n, ctypes.c_float) for n in floats] + [(n, ctypes.c_int32) for n in last]})
+
+
+Fp8Struct = _struct("Fp8Struct", ("values", "scales"), ("rows", "cols", "ld", "ld_scales"), ("rows_per_scale", "format"))
+CacheStruct = _struct("CacheStruct", ("k_codes", "v_codes", "k_grids", "v_grids"), ("pages",), ("page_size", "heads", "head_dim", "reserved"))
+BatchStruct = _struct("BatchStruct", ("table", "lengths", "starts"), ("rows", "table_ld"), ("n_seqs", "max_pages"))
+QueryStruct = _struct("QueryStruct", ("Q", "out", "lse"), ("q_row", "q_head", "out_row", "out_head", "max_length"), ("type", "group", "causal", "window"),
+                      ("scale",), ("reserved",))

@@ -247,15 +247,15 @@ def test_refusals(ctx):
         ctx.fp8_from_codes(codes, s[:, :1].contiguous(), s[:, :1].contiguous(), bits=8)
     lib = fobq.load_library()
     import ctypes
-    a = fobq.binding._fp8(ctx.handle, m, "A")
+    a = ref.Fp8Struct.from_buffer_copy(fobq.binding._fp8(ctx.handle, m, "A")[0])
     y = torch.zeros((4, 4), device="cuda")
     call = lambda a, b, ld: lib.fobq_fp8_matmul(ctx.handle, ctypes.byref(a), ctypes.byref(b), y.data_ptr(), 0, ld, None, 0)  # noqa: E731
     assert call(a, a, 4) == fobq.OK and call(a, a, 3) == fobq.EINVAL
     for field, value in [("rows", -1), ("cols", 257), ("ld", 250), ("ld_scales", 3), ("rows_per_scale", 2), ("format", 2), ("values", None), ("scales", None)]:
-        b = fobq.binding._fp8(ctx.handle, m, "B")
+        b = ref.Fp8Struct.from_buffer_copy(fobq.binding._fp8(ctx.handle, m, "B")[0])
         setattr(b, field, value)
         assert call(a, b, 4) == fobq.EINVAL, field
-    big = fobq.binding._fp8(ctx.handle, m, "A")
+    big = ref.Fp8Struct.from_buffer_copy(fobq.binding._fp8(ctx.handle, m, "A")[0])
     need = ctypes.c_int64(0)
     assert lib.fobq_fp8_matmul_workspace(ctx.handle, 128, 128, 1 << 20, 1, ctypes.byref(need)) == fobq.OK and need.value > 0
     assert lib.fobq_fp8_matmul_workspace(ctx.handle, 1, -1, 128, 1, ctypes.byref(need)) == fobq.EINVAL

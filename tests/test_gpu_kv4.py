@@ -475,7 +475,7 @@ def test_refusals(ctx):
         with pytest.raises(fobq.FobqError) as e:
             ctx.kv4_read(fobq.Kv4Cache.empty(pages, heads, dim, page), c.batch(), 2)
         assert e.value.code == fobq.EINVAL
-    cc, bb = fobq.binding._kv4(ctx.handle, c.cache, c.batch(), 2)
+    cc, bb = (t.from_buffer_copy(x) for t, x in zip((ref.CacheStruct, ref.BatchStruct), fobq.binding._kv4(ctx.handle, c.cache, c.batch(), 2)))
     lib = fobq.load_library()
     z = torch.zeros((2, 2, 128), dtype=BF, device="cuda")
     call = lambda: lib.fobq_kv4_append(ctx.handle, ctypes.byref(cc), ctypes.byref(bb), 1, z.data_ptr(), 256, 128, z.data_ptr(), 256, 128)  # noqa: E731
@@ -487,9 +487,9 @@ def test_refusals(ctx):
         assert call() == fobq.EINVAL, field
         setattr(s, field, old)
     long = Case(ctx, [(3000, 1)], 1, 128, 64)
-    cc, bb = fobq.binding._kv4(ctx.handle, long.cache, long.batch(), 1)
+    cc, bb = (t.from_buffer_copy(x) for t, x in zip((ref.CacheStruct, ref.BatchStruct), fobq.binding._kv4(ctx.handle, long.cache, long.batch(), 1)))
     qq = long.queries(1).cuda()
-    d = fobq.binding.FobqKv4Query(qq.data_ptr(), qq.data_ptr(), None, 128, 128, 128, 128, 0, 1, 1, 1, 0, 1.0, 0)
+    d = ref.QueryStruct(qq.data_ptr(), qq.data_ptr(), None, 128, 128, 128, 128, 0, 1, 1, 1, 0, 1.0, 0)
     need = ctypes.c_int64(0)
     assert lib.fobq_kv4_attention_workspace(ctx.handle, ctypes.byref(cc), ctypes.byref(bb), ctypes.byref(d), ctypes.byref(need)) == fobq.OK and need.value > 0
     assert lib.fobq_kv4_attention(ctx.handle, ctypes.byref(cc), ctypes.byref(bb), ctypes.byref(d), None, 0) == fobq.EINVAL
