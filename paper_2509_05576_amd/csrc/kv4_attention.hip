@@ -36,8 +36,8 @@ constexpr int VALUE_FLOOR = -60;
 constexpr float BIAS = 28.f, BIAS2 = 268435456.f;       // and 2^BIAS
 constexpr float RAISE = 8.f;            // binary orders of magnitude that a score may exceed the running maximum by
 constexpr int KV4_PART = 256;           // tokens of a part at least: eight tiles, two for each wavefront that shares the rows
-// Sequences of no more tokens than these are not split: one launch, not two, and no scratch.  (8 of 600 tokens, from call to call: 13 us,
-// 18 split; 32 of 1024: 16, 19.  At 2048 it turns: 16 sequences 20 us either way, 8 with 8 new tokens each 24, 19 split.)
+// Sequences of no more tokens than these are not split: one launch, not two, and no scratch.  (8 of 600 tokens, from call to call: 11 us,
+// 16 split; 32 of 1024: 16, 18.  At 2048 it turns: 16 sequences 19.5 us, 18.3 split; 8 with 8 new tokens each 24, 18.)
 constexpr int KV4_UNSPLIT = 1024;
 constexpr int KV4_MAX_PARTS = 64;       // a lane each where they are joined
 constexpr int KV4_SPLIT_SEQS = 256;     // more sequences than these are not split: they fill the chip
