@@ -450,16 +450,28 @@ class Fp8Matrix:
 
 def _fp8(ctx: int, m: Fp8Matrix, what: str):
     """What the library calls a matrix, its rows and columns."""
-    v, s, per = _need(m.values, ctx, _FP8, 2, what + ".values"), _need(m.scales, ctx, _F32, 2, what + ".scales"), m.rows_per_scale
-    (rows, cols), (sc, sr) = v.shape, s.shape
+    v, s, per, home = m.values, m.scales, m.rows_per_scale, _streams.get(ctx)
+    dev = home[0] if home is not None else None
+    try:
+        (ld, one), (ld_scales, one_scale), (rows, cols), (sc, sr) = v.stride(), s.stride(), v.shape, s.shape
+        fine = (v.dtype in _FP8 and s.dtype is torch.float32 and v.get_device() == dev and s.get_device() == dev and (one == 1 or cols <= 1)
+                and (one_scale == 1 or sr <= 1))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        # which of them it is
+        _need(v, ctx, _FP8, 2, what + ".values")
+        _need(s, ctx, _F32, 2, what + ".scales")
+        (ld, _), (ld_scales, _), (rows, cols), (sc, sr) = v.stride(), s.stride(), v.shape, s.shape
     wide = (cols + 15) & -16
     if per not in (1, 128) or sc != (cols + 127) // 128 or sr != (rows + per - 1) // per:
         raise TypeError(f"{what}: rows_per_scale must be 1 or 128 and scales (ceil(cols / 128), ceil(rows / rows_per_scale)), "
                         f"got {per} and {(sc, sr)} for {rows} x {cols}")
-    ld = v.stride()[0] if rows > 1 and cols else wide
+    if rows <= 1 or not cols:
+        ld = wide
     if wide != cols and rows and v.storage_offset() + (rows - 1) * ld + wide > v.untyped_storage().nbytes():
         raise TypeError(f"{what}: the last row must be readable to a multiple of 16 bytes")
-    return _fp8_matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, s.stride()[0] if sc > 1 else sr, per, _FP8[v.dtype]), rows, cols
+    return _fp8_matrix(v.data_ptr(), s.data_ptr(), rows, cols, ld, ld_scales if sc > 1 else sr, per, _FP8[v.dtype]), rows, cols
 
 
 def _new_fp8(ctx: int, rows: int, cols: int, format: torch.dtype, per: int, device):
@@ -599,12 +611,22 @@ def _kv4(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int):
 
 
 def _kv_rows(ctx: int, heads: int, dim: int, k: torch.Tensor, v: torch.Tensor, rows: int, dtypes):
-    shape = _need(k, ctx, dtypes, 3, "k").shape
-    _need(v, ctx, dtypes, 3, "v")
-    if v.shape != shape or k.dtype != v.dtype or shape != (rows, heads, dim):
-        raise TypeError(f"k and v: need {(rows, heads, dim)} of one type, got {tuple(shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
-    (k_row, k_head, _), (v_row, v_head, _) = k.stride(), v.stride()
-    return (_FLOAT[k.dtype], k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head)
+    home, shape = _streams.get(ctx), (rows, heads, dim)
+    dev = home[0] if home is not None else None
+    try:
+        (k_row, k_head, one), (v_row, v_head, one_v), dtype = k.stride(), v.stride(), k.dtype
+        fine = (dtype in dtypes and v.dtype is dtype and k.shape == shape and v.shape == shape and one == 1 and one_v == 1 and k.get_device() == dev
+                and v.get_device() == dev)
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        # which of them it is
+        _need(k, ctx, dtypes, 3, "k")
+        _need(v, ctx, dtypes, 3, "v")
+        if k.shape != shape or v.shape != shape or k.dtype != v.dtype:
+            raise TypeError(f"k and v: need {shape} of one type, got {tuple(k.shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
+        (k_row, k_head, _), (v_row, v_head, _), dtype = k.stride(), v.stride(), k.dtype
+    return (_FLOAT[dtype], k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head)
 
 
 def fobq_kv4_append(ctx: int, cache: Kv4Cache, batch: Kv4Batch, k: torch.Tensor, v: torch.Tensor) -> None:
