@@ -435,7 +435,9 @@ def _empty(ctx: int, shape, dtype: torch.dtype, device) -> torch.Tensor:
     home = _streams.get(ctx)
     if home is None or _current_stream(device.index) == home[1]:
         return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(torch.cuda.ExternalStream(home[1], device=device)):
+    # (the default stream has no handle: torch takes an external stream of 0 as one that is not given, and makes another)
+    stream = torch.cuda.ExternalStream(home[1], device=device) if home[1] else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
