@@ -49,12 +49,12 @@ __device__ __forceinline__ float fp8_quotient(const Fp8Scale& s, float x)
     return fmaf(fmaf(x, s.pre, -p) - e, s.corr, y);
 }
 // A quotient y that lies on a border, or not: one step to the side on which x / scale lies if that is not y itself.  (The remainder's sign is
-// exact; an odd fp32 number is on no border.)
+// exact; an odd fp32 number is on no border, nor is 0, which a value far below the smallest one gives.)
 __device__ __forceinline__ float fp8_side(const Fp8Scale& s, float x, float y)
 {
     const float p = y * s.most, rest = fmaf(x, s.pre, -p) - fmaf(y, s.most, -p);
     const uint32_t bits = __float_as_uint(y);
-    if (s.most == 0.f || rest == 0.f || (bits & 1)) return y;          // (most 0: y is exact, or NaN)
+    if (s.most == 0.f || rest == 0.f || (bits & 1) || bits << 1 == 0) return y;          // (most 0: y is exact, or NaN)
     return __uint_as_float(bits + ((rest > 0.f) == (y > 0.f) ? 1 : -1));
 }
 
