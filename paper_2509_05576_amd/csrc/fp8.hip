@@ -6,7 +6,9 @@
 // The quotient: with top = 0.875 * 2^9 or * 2^16, x / (most / top) = (0.875 x) / (most / 2^9 or 2^16); one multiplication by the reciprocal
 // and one correction from the remainder round it to fp32 as a division would.  Where that lies on the border of two 8-bit values (one of 2^20
 // fp32 quotients, and zeros) the remainder says on which side the quotient lies, so that it is rounded to 8 bits once and not twice.  It
-// never passes the largest value by more than a rounding, which the conversion takes back.
+// never passes the largest value by more than a rounding, which the conversion takes back.  The remainder has bits 2^-47 below x: blocks
+// whose largest is below 2^-40 are taken 2^80 times as large on both sides, so that those are not below what fp32 holds for any x that does not
+// round to 0 (that is, above 2^-33 of the largest).
 #include "lowbit.h"
 
 namespace fobq {
@@ -39,8 +41,8 @@ __device__ __forceinline__ Fp8Scale fp8_scale(uint32_t bits)
     const float most = __uint_as_float(bits), scale = most / Fp8<FORMAT>::TOP;
     if (bits >= 0x7f800000u) return Fp8Scale{__builtin_nanf(""), __builtin_nanf(""), 0.f, 1.f, 0.f};
     if (scale < FP8_TINY) return Fp8Scale{FP8_TINY, 1.f, 0.f, 0x1p126f, 0.f};
-    const float m = most * Fp8<FORMAT>::POW, inv = 1.f / m;
-    return Fp8Scale{scale, 0.875f, m, inv, inv};
+    const float lift = most < 0x1p-40f ? 0x1p80f : 1.f, m = most * lift * Fp8<FORMAT>::POW, inv = 1.f / m;
+    return Fp8Scale{scale, 0.875f * lift, m, inv, inv};
 }
 // x / scale, rounded once: the remainder of the first guess is exact (its product's error is taken along, and what is left of x fits)
 __device__ __forceinline__ float fp8_quotient(const Fp8Scale& s, float x)

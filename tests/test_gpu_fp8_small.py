@@ -44,3 +44,32 @@ def test_values_that_vanish_beside_a_large_one(ctx, fmt, per, dtype):
     # and through a product: the row that holds them is finite
     y = ctx.fp8_matmul(ctx.fp8_quantize(x[:, :640].contiguous().cuda(), fmt), ctx.fp8_quantize(torch.ones((3, 640), device="cuda")), torch.float32)
     assert y.isfinite().all()
+
+
+@pytest.mark.parametrize("power", [-30, -41, -60, -90, -110, -117])
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("per", [1, 128])
+def test_quotients_beside_a_border_in_blocks_of_small_values(ctx, fmt, per, power):
+    """Quotients on the border of two 8-bit values, or by it, closer than fp32 tells apart, where the block's largest is 2^power: the side is
+    the exact quotient's (x * top against border * largest, both exact in 64 bits), ties to the even one."""
+    top, keep = (448.0, 3) if fmt == E4 else (57344.0, 2)
+    g = torch.Generator().manual_seed(per - power)
+    most = ((torch.rand((1 if per == 128 else 128, 1), generator=g) + 1.0) * 2.0 ** power).expand(128, 1).contiguous()
+    most = most.clamp(min=top * 2.0 ** -125)                       # (below it the scale is the smallest one, not the largest value's)
+    low = -6 if fmt == E4 else -14
+    power_of = 2.0 ** torch.randint(low - 1, 8, (128, 512), generator=g).double()
+    steps, at_least = torch.randint(0, 2 ** keep, (128, 512), generator=g).double(), power_of.clamp(min=2.0 ** low)
+    below = torch.where(power_of < at_least, steps * at_least / 2 ** keep, (2 ** keep + steps) * at_least / 2 ** keep)
+    above = below + at_least / 2 ** keep
+    border = (below + above) / 2
+    x = (border * most.double() / top).float()
+    near = torch.stack((x, torch.nextafter(x, x * 2), torch.nextafter(x, x * 0)))
+    x = near.gather(0, torch.randint(0, 3, (1, 128, 512), generator=g))[0]
+    last = torch.arange(512) % 128 == 127                          # each block's largest, in its last place
+    x[:, last] = most.expand(-1, 4)
+    x = x * torch.where(torch.rand((128, 512), generator=g) < 0.5, -1.0, 1.0)
+    got = ctx.fp8_quantize(x.cuda(), fmt, per).values.cpu().double()
+    q, m = x.double().abs() * top, border * most.double()
+    want = torch.where((q > m) | ((q == m) & (steps % 2 == 1)), above, below) * x.sign()
+    assert torch.equal(got[:, ~last], want[:, ~last])
+    assert (got[:, last].abs() == top).all()
