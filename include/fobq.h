@@ -312,7 +312,8 @@ typedef struct {
  * 0 .. rows; NULL: one row each, row i) and holds lengths[i] tokens, those of its rows included: they are its last ones, in order.
  * Token t of it lies in page table[i * table_ld + t / page_size] at place t % page_size.  Rows behind the last
  * sequence are not touched.  An entry outside 0 .. pages - 1 is no page: nothing is written there and its tokens are not there; so
- * are tokens behind max_pages pages and rows whose token would come before token 0.  No address is formed from either. */
+ * are tokens behind max_pages pages and rows whose token would come before token 0.  No address is formed from either.  (A row whose own token
+ * is not there is not stored and reads 0, and attends to those tokens that it would see and that are there.) */
 typedef struct {
     const int32_t* table;      /* device, n_seqs x max_pages, row stride table_ld                         */
     const int32_t* lengths;    /* device, n_seqs                                                          */

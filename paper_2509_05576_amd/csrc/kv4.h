@@ -30,12 +30,10 @@ __host__ __device__ inline Kv4Rows kv4_rows(const int32_t* starts, int b, int ro
     return Kv4Rows{lo, hi - lo};
 }
 
-// Tokens that sequence b holds, kept inside its table.
-__host__ __device__ inline int kv4_length(const int32_t* lengths, int b, int max_pages, int shift)
-{
-    const int64_t n = lengths[b], most = (int64_t)max_pages << shift;
-    return (int)(n < 0 ? 0 : (n > most ? most : n));
-}
+// Tokens of sequence b, as the caller says (its new rows are the last of them), and the most that its table has places for: those behind
+// are not there.
+__host__ __device__ inline int kv4_length(const int32_t* lengths, int b) { return lengths[b] < 0 ? 0 : lengths[b]; }
+__host__ __device__ inline int kv4_places(int max_pages, int shift) { return max_pages << shift; }       // below 2^30
 
 // Where packed row `row` of sequence b lies: its page (-1: none) and its place there.
 struct Kv4Place { int page, place; };
@@ -43,7 +41,7 @@ __host__ __device__ inline Kv4Place kv4_place(const Kv4Seqs& s, int pages, int s
 {
     const Kv4Rows r = kv4_rows(s.starts, b, s.rows);
     if (row < r.first || row >= r.first + r.count) return Kv4Place{-1, 0};
-    const int t = kv4_length(s.lengths, b, s.max_pages, shift) - r.count + (row - r.first);
+    const int t = kv4_length(s.lengths, b) - r.count + (row - r.first);
     if (t < 0) return Kv4Place{-1, 0};
     return Kv4Place{kv4_page(s.table + (int64_t)b * s.table_ld, s.max_pages, pages, shift, t), t & ((1 << shift) - 1)};
 }

@@ -88,8 +88,9 @@ __device__ __forceinline__ Split split_of(const AttnArgs& a)
             const Kv4Rows r = kv4_rows(a.s.starts, b, a.s.rows);
             s.row[j] = r.first;
             s.count[j] = r.count;
-            s.length[j] = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
-            const int tokens = a.q.window > 0 ? (int)min((int64_t)s.length[j], (int64_t)a.q.window + r.count) : s.length[j];
+            s.length[j] = kv4_length(a.s.lengths, b);
+            const int held = min(s.length[j], kv4_places(a.s.max_pages, a.c.shift));
+            const int tokens = a.q.window > 0 ? (int)min((int64_t)held, (int64_t)a.q.window + r.count) : held;
             tiles[j] = (r.count * a.q.group + a.tile - 1) / a.tile;
             spans[j] = (tokens + 31) / 32;
             // (starts out of order could make more tiles than there are slots: those are cut off, here and where they are joined)
@@ -332,7 +333,7 @@ __device__ __forceinline__ Ranked ranked(const AttnArgs& a, int tile_rows, int i
             const Kv4Rows r = kv4_rows(a.s.starts, b, a.s.rows);
             row[j] = r.first;
             count[j] = r.count;
-            length[j] = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
+            length[j] = kv4_length(a.s.lengths, b);
             tiles[j] = (int)(((int64_t)r.count * a.q.group + tile_rows - 1) / tile_rows);
             base[j] = (int)min((int64_t)max(0, length[j] - r.count) * a.q.group / tile_rows, (int64_t)(1 << 30) - 1);
             top = max(top, base[j] + tiles[j]);
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         const int place = SHARE ? index : (int)(gridDim.x / a.c.heads) - 1 - index;
         b = __builtin_amdgcn_readfirstlane(wave_search(a.s.n_seqs, place, first_tile));
         mine = kv4_rows(a.s.starts, b, a.s.rows);
-        length = kv4_length(a.s.lengths, b, a.s.max_pages, a.c.shift);
+        length = kv4_length(a.s.lengths, b);
         tile_of_rows = (int)max((int64_t)-1, place - first_tile(b));
     }
     const int rows = mine.count * G;                                   // tokens x query heads of the kv head
@@ -479,7 +480,11 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     const int before = length - mine.count;                            // position of the sequence's first new token (< 0: it is not there)
     const int32_t* __restrict__ table = a.s.table + (int64_t)b * a.s.table_ld;
 
-    // the tokens that each of this lane's rows sees, [from, to), and those that all / any of the wavefront's rows see
+    // the tokens that each of this lane's rows sees, [from, to), and those that all / any of the wavefront's rows see: windows by the rows'
+    // own tokens, which may lie behind the table, and no token behind the table
+    const int places = kv4_places(a.s.max_pages, a.c.shift);
+    auto end_of = [&](int i) { return a.q.causal ? before + i + 1 : length; };        // new token i's
+    auto start_of = [&](int i) { return a.q.window > 0 ? max(0, end_of(i) - a.q.window) : 0; };
     int from[QT], to[QT];
     u4 qf[QT][D / 32];
     float qsum[QT];
@@ -488,8 +493,8 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         const int rho = base + 16 * t + col;
         const bool there = rho < rows;
         const int i = there ? rho / G : 0, hq = there ? rho - i * G : 0;
-        to[t] = there ? (a.q.causal ? before + i + 1 : length) : 0;
-        from[t] = a.q.window > 0 ? max(0, to[t] - a.q.window) : 0;
+        to[t] = there ? min(places, end_of(i)) : 0;
+        from[t] = start_of(i);
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
@@ -513,17 +518,16 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
         qsum[t] = quarters_sum(sum);
     }
     // what any of the wavefront's rows sees, and what all of them see (rows that are not there may see what they like)
-    const int last = max(base, min(base + 16 * QT, rows) - 1);
-    const int to0 = a.q.causal ? before + base / G + 1 : length, to1 = a.q.causal ? before + last / G + 1 : length;
-    int any_to = base < rows ? max(0, to1) : 0, all_to = to0;
-    const int any_from = a.q.window > 0 ? max(0, to0 - a.q.window) : 0, all_from = a.q.window > 0 ? max(0, to1 - a.q.window) : 0;
+    const int row0 = min(base, rows - 1) / G, row1 = (min(base + 16 * QT, rows) - 1) / G;
+    int any_to = base < rows ? max(0, min(places, end_of(row1))) : 0, all_to = min(places, end_of(row0));
+    const int any_from = start_of(row0), all_from = start_of(row1);
 
     // this part's tokens, in tiles of 32; without SHARE the workgroup's rows, and `needed` those tiles that the wavefront's see
     int wg_from = any_from, wg_to = any_to;
     if constexpr (!SHARE) {
         const int first = (int)base64, final = min(first + TILE, rows) - 1;
-        wg_to = max(0, a.q.causal ? before + final / G + 1 : length);
-        wg_from = a.q.window > 0 ? max(0, (a.q.causal ? before + first / G + 1 : length) - a.q.window) : 0;
+        wg_to = max(0, min(places, end_of(final / G)));
+        wg_from = start_of(first / G);
     }
     const int tile0 = wg_from / 32, tile1 = (wg_to + 31) / 32;
     const int per = (max(0, tile1 - tile0) + parts - 1) / parts;
