@@ -484,7 +484,8 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     // own tokens, which may lie behind the table, and no token behind the table
     const int places = kv4_places(a.s.max_pages, a.c.shift);
     auto end_of = [&](int i) { return a.q.causal ? before + i + 1 : length; };        // new token i's
-    auto start_of = [&](int i) { return a.q.window > 0 ? max(0, end_of(i) - a.q.window) : 0; };
+    // (a row before token 0 has an end below 0, from which a wide window would pass 32 bits)
+    auto start_of = [&](int i) { return a.q.window > 0 ? max(0, max(0, end_of(i)) - a.q.window) : 0; };
     int from[QT], to[QT];
     u4 qf[QT][D / 32];
     float qsum[QT];

@@ -85,3 +85,16 @@ def test_attention(ctx, form, over, causal, window):
             assert (lse[at:at + new, hq][~seen] == -math.inf).all()
             assert ((lse[at:at + new, hq] - wl).abs()[seen] <= lbound[seen]).all()
         at += new
+
+
+@pytest.mark.parametrize("seqs,group,dim", [([(2, 10), (40, 3)], 2, 128), ([(30, 100)], 1, 64), ([(1500, 1600)], 1, 128), ([(1500, 3), (4, 20)], 1, 128)])
+def test_rows_before_token_0_under_a_window_beyond_every_length(ctx, seqs, group, dim):
+    """Few rows, prompts, and split sequences: the rows before token 0 see nothing, the others all that is there up to their own."""
+    c = Case(ctx, seqs, 1, dim, 16, BF, seed=dim)
+    q = c.queries(group).cuda()
+    lse = torch.empty((c.rows, group), device="cuda")
+    want = ctx.kv4_attention(c.cache, c.batch(), q, lse=lse)
+    for window in ((1 << 31) - 1, (1 << 31) - 5, (1 << 31) - 9, 1 << 30, 5000):
+        got_lse = torch.empty_like(lse)
+        assert torch.equal(ctx.kv4_attention(c.cache, c.batch(), q, window=window, lse=got_lse), want) and torch.equal(lse, got_lse), window
+    assert (want[:max(0, seqs[0][1] - seqs[0][0])] == 0).all() and not (want[-1] == 0).all()
