@@ -79,7 +79,11 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4View c, Kv4Seqs s, c
         hi = over_lanes<LANES>(hi, [](float a, float b) { return fmaxf(a, b); });
         bad = over_lanes<LANES>(bad, [](float a, float b) { return a + b; });
         if (h >= c.heads) continue;
-        const float range = (hi - lo) / 15.f;
+        // the range, rounded up: next to an end of 15 bf16 steps the other end may be too small for fp32 to add, and counts all the same
+        float range = hi - lo;
+        const float larger = fmaxf(hi, -lo);
+        if (fminf(hi, -lo) > range - larger) range = __uint_as_float(__float_as_uint(range) + 1);
+        range /= 15.f;
         float scale = __uint_as_float((__float_as_uint(range) + 0xffffu) & 0xffff0000u);
         scale = fmaxf(scale, KV4_TINY);
         uint32_t word = 0;
