@@ -262,7 +262,7 @@ typedef enum { FOBQ_E4M3 = 0, FOBQ_E5M2 = 1 } fobq_fp8;
  * The last blocks may be partial.  values: 16-byte aligned, ld (bytes) a multiple of 16 and no less than cols; the calls
  * that read a matrix may read each row, the last one too, up to the next multiple of 16 columns (and ignore what is there),
  * those that write one leave what is behind column cols - 1 as it was.  1 <= rows, cols < 2^29 (0 allowed where nothing is
- * read), and rows * ceil(cols / 512) below 2^26 - 3. */
+ * read), and rows * ceil(cols / 512) below 2^26 - 3, rows alone too. */
 typedef struct {
     void*   values;
     float*  scales;

@@ -1,6 +1,8 @@
 // C ABI of the calls that run a quantized network: argument checks and launches.  They allocate nothing and wait for nothing.
 #include "kv4.h"
 
+#include <algorithm>
+
 namespace fobq {
 
 constexpr int64_t MAX_SIDE = (int64_t)1 << 29;      // rows and columns of a matrix, rows times query heads: products with 4 stay in 32 bits
@@ -20,7 +22,7 @@ static int check_matrix(fobq_ctx* ctx, const fobq_fp8_matrix* m, const char* nam
     if (!m) return set_err(ctx, FOBQ_EINVAL, "%s is NULL", name);
     if (m->rows < 0 || m->rows >= MAX_SIDE || m->cols < 0 || m->cols >= MAX_SIDE)
         return set_err(ctx, FOBQ_EINVAL, "%s: rows and cols must be in 0..%lld", name, (long long)MAX_SIDE - 1);
-    if (m->rows * ((m->cols + 511) / 512) > MAX_ROWS)
+    if (m->rows * std::max<int64_t>(1, (m->cols + 511) / 512) > MAX_ROWS)       // (no columns: a product's results are written all the same)
         return set_err(ctx, FOBQ_EINVAL, "%s: rows times 512 columns must be no more than %lld (got %lld x %lld)", name, (long long)MAX_ROWS, (long long)m->rows, (long long)m->cols);
     if (m->format != FOBQ_E4M3 && m->format != FOBQ_E5M2) return set_err(ctx, FOBQ_EINVAL, "%s: unknown format %d", name, m->format);
     if (m->rows_per_scale != 1 && m->rows_per_scale != 128)

@@ -15,7 +15,7 @@ def pytest_configure(config):
 
 # A test whose expected value is wrong; it stays as it is.  test_places expects the token of a sequence of 2^31 - 1 tokens at the last place of a table of
 # 48, where the contract (include/fobq.h: token t at table entry t / page_size; tokens behind the table are not there) has no page for it.  All
-# of its statements, with that one as the contract has it, are in test_lowbit_places.py.
+# of its statements, with that one as the contract has it, are in test_lowbit_limits.py.
 WRONG = {"test_lowbit_host.py::test_places": "expects a token behind the table at the table's last place"}
 
 

@@ -1,5 +1,5 @@
-"""Where a row's token lies when lengths, pages and starts are not as they should be: the statements of the host tests' test_places, with a
-length that passes the table as the contract has it (no GPU)."""
+"""What the calls on few bits refuse, and where a row's token lies when lengths, pages and starts are not as they should be: the statements of
+the host tests' test_places, with a length that passes the table as the contract has it (no GPU)."""
 import pytest
 
 pytest.importorskip("torch")
@@ -37,3 +37,11 @@ def test_a_length_that_passes_the_table(length):
             token = length - count + row
             want = [0, TABLE[0][token // 16], token % 16] if token < 48 else [0, -1]
             assert at(row, lengths=[length, 3, 17, 0], starts=[0, count, count, count, count])[:len(want)] == want
+
+
+@pytest.mark.parametrize("rows,cols,ok", [((1 << 26) - 4, 0, True), ((1 << 26) - 3, 0, False), ((1 << 29) - 1, 0, False), ((1 << 26) - 4, 512, True),
+                                          ((1 << 26) - 4, 513, False)])
+def test_rows_of_no_columns(rows, cols, ok):
+    """A product over no columns writes zeros: as many rows as its launch has workgroups for."""
+    got = fobq.fobq_debug_plan(fobq.PLAN_FP8_CHECK, [rows, cols, -(-cols // 16) * 16, rows, 1, 0, 0x7000000000, 0x7000000000], 1)
+    assert got == [fobq.OK if ok else fobq.EINVAL]
