@@ -106,6 +106,8 @@ int lowbit_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* ou
     if (what == FOBQ_PLAN_KV4_PLACE && n_in >= 6 && n_out == 3) {
         const int64_t n = in[3], width = in[2];
         if (n < 1 || n > 64 || width < 0 || width > 64 || n_in != 6 + n + n + 1 + n * width) return FOBQ_EINVAL;
+        if (in[0] < 16 || in[0] > 4096 || (in[0] & (in[0] - 1)) || in[1] < 1 || in[1] > INT32_MAX || in[4] < 0 || in[4] > MAX_ROWS || in[5] < 0 ||
+            in[5] > MAX_ROWS) return FOBQ_EINVAL;
         int32_t lengths[64], starts[65], table[64 * 64];
         for (int i = 0; i < n; ++i) lengths[i] = (int32_t)in[6 + i];
         for (int i = 0; i <= n; ++i) starts[i] = (int32_t)in[6 + n + i];

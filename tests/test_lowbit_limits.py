@@ -45,3 +45,10 @@ def test_rows_of_no_columns(rows, cols, ok):
     """A product over no columns writes zeros: as many rows as its launch has workgroups for."""
     got = fobq.fobq_debug_plan(fobq.PLAN_FP8_CHECK, [rows, cols, -(-cols // 16) * 16, rows, 1, 0, 0x7000000000, 0x7000000000], 1)
     assert got == [fobq.OK if ok else fobq.EINVAL]
+
+
+@pytest.mark.parametrize("change", [dict(page=0), dict(page=8), dict(page=24), dict(page=8192), dict(page=(1 << 62) + 1), dict(page=2 ** 63 - 1), dict(page=-16),
+                                    dict(pages=0), dict(pages=1 << 31), dict(rows=-1), dict(rows=1 << 40), dict(row=-1), dict(row=1 << 33)])
+def test_places_are_asked_of_caches_that_there_can_be(change):
+    with pytest.raises(fobq.FobqError):
+        at(**{"row": 0, **change})
