@@ -413,6 +413,7 @@ def fobq_debug_offset_tables(k: int, pad: int, h: int, w: int):
 # Like the entry points they wrap, these calls enqueue on the context's stream and return.  What they allocate (outputs that are not
 # given, scratch) belongs to that stream; inputs that another stream made, and outputs that another stream uses, are ordered by the
 # caller, as between any two streams.  Under capture the context's stream has to be the captured one.
+# They have no backward pass: tensors that require gradients are taken as they are, and results do not require any.
 # The checks of a call are a few attribute reads each: a call takes the host 3 us to launch, and a step of generation makes hundreds.
 _current_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
     lambda index: torch.cuda.current_stream(index).cuda_stream)      # (the public call makes a stream object: 1.9 us against 0.1)
@@ -497,7 +498,7 @@ def _out_fp8(ctx: int, out: Optional[Fp8Matrix], rows: int, cols: int, format: t
 
 def fobq_fp8_quantize(ctx: int, X: torch.Tensor, format: torch.dtype = torch.float8_e4m3fn, rows_per_scale: int = 1,
                       out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
-    """X: 2-D device tensor (fp32, bf16 or fp16) -> Fp8Matrix: rows_per_scale 1 for activations, 1 or 128 for weights."""
+    """X: 2-D device tensor (fp32, bf16 or fp16) -> Fp8Matrix: rows_per_scale 1 for activations, 1 or 128 for weights.  No gradient passes it."""
     _need(X, ctx, _FLOAT, 2, "X")
     rows, cols = X.shape
     out, m = _out_fp8(ctx, out, rows, cols, format, rows_per_scale, X.device)
@@ -528,7 +529,8 @@ def _scratch(ctx: int, need: int, device) -> Optional[torch.Tensor]:
 
 
 def fobq_fp8_matmul(ctx: int, A: Fp8Matrix, B: Fp8Matrix, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """A (activations, m x k) times B (weights, n x k) transposed -> m x n of `dtype` (fp32, bf16 or fp16), or into `out`."""
+    """A (activations, m x k) times B (weights, n x k) transposed -> m x n of `dtype` (fp32, bf16 or fp16), or into `out`.  In 16 bits, rows beyond
+    16 take the 8-bit matrix unit, whose sums of eight products keep 13 bits below the largest; up to 16 rows, and fp32, sum in fp32."""
     (a, m, k), (b, n, k2) = _fp8(ctx, A, "A"), _fp8(ctx, B, "B")
     if k != k2:
         raise TypeError(f"A has {k} columns, B {k2}")
@@ -654,7 +656,8 @@ def fobq_kv4_read(ctx: int, cache: Kv4Cache, batch: Kv4Batch, rows: int, dtype: 
 def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tensor, *, scale: Optional[float] = None, causal: bool = True,
                        window: int = 0, max_length: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
     """q (bf16 or fp16, rows x query heads x head_dim) over the sequences' tokens -> the same shape, or into `out`.  scale: head_dim^-0.5
-    unless given.  max_length: the most tokens a sequence holds, if known (a hint).  lse (fp32, rows x query heads): filled."""
+    unless given.  max_length: the most tokens a sequence holds, if known (a hint).  lse (fp32, rows x query heads): filled.  No gradient passes
+    it.  Rows of no sequence stay as they are, uninitialized in a new result."""
     _need(q, ctx, _HALF, 3, "q")
     rows, heads_q, dim = q.shape
     c, b, heads, channels = _kv4(ctx, cache, batch, rows)

@@ -1,6 +1,7 @@
 // Product of two matrices in 8-bit floating point with a scale for each block of 128 columns:
 //   Y[m][n] = sum_kb sa[kb][m] sb[kb][n / per] sum_{k in block kb} A[m][k] B[n][k]
-// The outer sum is a multiply-add per value and block on the vector units, in fp32: acc += (sa sb) * part.  The inner one is
+// The outer sum is a multiply-add per value and block on the vector units, in fp32: acc += (sa sb) * part, or, with a scale per row of B, acc +=
+// sa * (sb * part) (scales whose product or whose product with a part passes fp32 give what fp32 gives).  The inner one is
 //   one 16x16x128 matrix instruction on 8-bit operands (its own scales at 1) for results in 16 bits.  That instruction adds the products
 //     of eight neighbouring k's to 13 bits below the largest of them before its fp32 sums (measured: a product of 2^-14 of the largest is
 //     lost, from another eight it is kept to 2^-23): 1.5e-5 of a block's result on Gaussian values, 5.5e-5 where they spread over

@@ -54,8 +54,9 @@ struct AttnArgs {
 };
 
 // How the sequences are split into parts of about equal size, which the host cannot know: the lengths are on the device.  A sequence has
-// one workgroup per tile of its rows and part of its tokens; the longest part is as short as it can be with all of them in the slots
-// that there are, which the chip holds at a time.  Every wavefront works this out for itself, a lane to a sequence.  (32 sequences of 5000 to
+// one workgroup per tile of its rows and part of its tokens, up to KV4_MAX_PARTS parts of KV4_PART tokens at least; the longest part is
+// about as short as it can be with all of them in the slots that there are, which the chip holds at a time (six halvings: to 1 / 64 of the
+// distance between a length that is too short and one that fits for sure).  Every wavefront works this out for itself, a lane to a sequence.  (32 sequences of 5000 to
 // 16000 tokens in as many parts each take 88 us, so 82; 8 of 16384 in three times as many parts 48, so 40.)
 struct Split {
     static constexpr int J = KV4_SPLIT_SEQS / 64;
@@ -892,6 +893,8 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a)
 
 Kv4Plan kv4_attention_plan(int cus, int dim, int heads, int group, int n_seqs, int64_t rows, int64_t longest)
 {
+    // The form goes by the average: the host does not know a sequence's rows.  What it was chosen by are calls of sequences alike; where prompts
+    // and single tokens share a call, the one or the other runs in a form that is not its own (results are the same to rounding).
     Kv4Plan p;
     const int64_t each = n_seqs > 0 ? (rows * group + n_seqs - 1) / n_seqs : 0;     // rows of a sequence and kv head, on average
     p.share = each <= (dim == 256 ? 16 : 32);
