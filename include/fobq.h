@@ -344,9 +344,9 @@ int fobq_kv4_read(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv4_bat
  * A row sees, causal != 0: the tokens up to its own; 0: all of its sequence; of those, window > 0: the last `window`.  A row that
  * sees nothing is 0.  Scores, softmax and sums in fp32; the queries as given, the weights p in fp16 against the largest scale of the
  * values met, the result rounded once.  The same bits in every run on equal arguments.  What that leaves, beside the last rounding:
- *   weights times scales have 11 bits down to 2^-14 of the row's largest, lose bits below it, and add nothing to the result (but to the sum) below
- *     2^-25 of it: n such tokens of values |v| up to 15 scales may be missed by n 2^-25 of the largest;
- *   values whose scale is below 2^-60 count as if the largest met were no smaller than that, and lose bits from 2^-74 on;
+ *   weights times scales have 11 bits down to 2^-20 of the row's largest, lose bits below it, and add nothing to the result (but to the sum) below
+ *     2^-31 of it: n such tokens of values |v| up to 15 scales may be missed by n 2^-31 of the largest;
+ *   values whose scale is below 2^-60 count as if the largest met were no smaller than that, and lose bits from 2^-80 on;
  *   with BF16 queries the keys' codes enter the sums as 128 + code, and (128 + zero) times the sum of q is taken off again: a score's fp32 error is
  *     relative to up to 143 times the sum of |q| times the key's scale, where codes alone (F16 queries) have 15. */
 typedef struct {

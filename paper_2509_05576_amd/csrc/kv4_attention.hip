@@ -14,9 +14,10 @@
 // the lane transposes 8 tokens x dim / 16 codes by byte selects.  A lane's results are dim / 4 consecutive channels of one query row.
 //
 // fp16 weights and the range of V: m follows the running maximum of S + log2 scale_v (its whole part), not of S, so that a row's largest
-// weights are near 1 whatever the size of the values.  The sum of the softmax has the same m, raised by 2^28 (scale_v takes that off P again):
+// weights are near 1 whatever the size of the values, and enter fp16 2^6 up, where the largest still fit (below 2^15) and those down to 2^-20 of
+// it keep all 11 bits, the others down to 2^-31 some: a long tail behind a few strong tokens is made of such.  The sum of the softmax has the same m, raised by 2^28 (scale_v takes that off P again):
 // with scales up to 2^127 its largest terms are still 2^27 times what fp32 can hold, with scales down to 2^-60 2^31 of them are finite.
-// Smaller scales count as 2^-60 in m, so that values below 2^-74 lose bits.
+// Smaller scales count as 2^-60 in m, so that values below 2^-80 lose bits.
 // The maximum is raised only when it is exceeded by 2^8: most tiles of 32 tokens then rescale nothing.
 #include "kv4.h"
 
@@ -34,6 +35,7 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 constexpr float NEG_MAX = -3.402823466e38f;
 constexpr int VALUE_FLOOR = -60;
 constexpr float BIAS = 28.f, BIAS2 = 268435456.f;       // and 2^BIAS
+constexpr float LIFT = 64.f;            // what fp16 weights are taken up by: the largest is below 2 * 2^RAISE * LIFT = 2^15
 constexpr float RAISE = 8.f;            // binary orders of magnitude that a score may exceed the running maximum by
 constexpr int KV4_PART = 256;           // tokens of a part at least: eight tiles, two for each wavefront that shares the rows
 // Sequences of no more tokens than these are not split: one launch, not two, and no scratch.  (8 of 600 tokens, from call to call: 11 us,
@@ -616,7 +618,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
     };
     // the weights times the values' scales, and their sums
     auto weigh = [&](uint32_t v_grid, const float (&u)[QT][8], f16x8 (&p)[QT]) {
-        const float va = __uint_as_float(v_grid & 0xffff0000u) * (1.f / BIAS2);
+        const float va = __uint_as_float(v_grid & 0xffff0000u) * (LIFT / BIAS2);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             float w[8];
@@ -790,7 +792,7 @@ __global__ __launch_bounds__(256, 2) void kv4_attention_kernel(AttnArgs a)
             for (int j = 0; j < N / 4; ++j) dst[j] = f4{value(4 * j), value(4 * j + 1), value(4 * j + 2), value(4 * j + 3)};
             return;
         }
-        const float inv = ll == 0.f ? 0.f : BIAS2 / ll;                // a row that sees nothing is 0
+        const float inv = ll == 0.f ? 0.f : BIAS2 / LIFT / ll;                // a row that sees nothing is 0
         T out[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) out[k] = (T)(value(k) * inv);
@@ -883,7 +885,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(AttnArgs a)
 #pragma unroll
             for (int c = 0; c < N; ++c) y[c] += wp[k] * v[k][c];
     }
-    const float inv = sum == 0.f ? 0.f : BIAS2 / sum;
+    const float inv = sum == 0.f ? 0.f : BIAS2 / LIFT / sum;
     T out[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) out[c] = (T)(y[c] * inv);
