@@ -137,7 +137,7 @@ __device__ __forceinline__ void wait_and_meet()
 }
 
 // TM x TN outputs by WM x WN wavefronts, the tiles of STAGES - 1 blocks under way.  FA, FB: the types of A and B; PER: rows of B to a scale.
-// (8192^3, a scale per 128 x 128, bf16 results: 487 us, 2.26 PFLOP/s, with the matrix units busy for 51 % of the cycles and the vector units,
+// (8192^3, a scale per 128 x 128, bf16 results: 487 to 495 us, 2.26 PFLOP/s, with the matrix units busy for 51 % of the cycles and the vector units,
 // the sums' multiply-adds, for 48 % beside them, at a clock that power keeps near 2 GHz; a library's plain 8-bit product, without scales
 // of blocks, takes 411.  4096^3: 66 us; with a scale per row of B, a multiplication more for each sum, 95; EXACT 148.)
 template <int TM, int TN, int WM, int WN, int STAGES, int FA, int FB, int PER, bool EXACT>
