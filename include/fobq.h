@@ -368,6 +368,103 @@ int fobq_kv4_attention(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv
 int fobq_kv4_attention_workspace(fobq_ctx* ctx, const fobq_kv4_cache* cache, const fobq_kv4_batch* batch, const fobq_kv4_query* query,
                                  int64_t* bytes);
 
+/* A feed-forward part of experts.  A router sends each token to a few of many small networks, whose rows are products of 8-bit blocks as above.
+ * A layer of them is fobq_fp8_rms_norm, fobq_route, fobq_fp8_expert_matmul (packed 0), fobq_fp8_swiglu, fobq_fp8_expert_matmul (packed 1) and
+ * fobq_expert_sum; the first and the fourth stand in front of and between any products of 8-bit blocks. */
+
+/* The residual's addition and a root-mean-square norm, into 8-bit blocks.  Per row, in fp32 but for the sum of squares (fp64):
+ *   s = X + residual (X without one),  y = s / sqrt(mean(s^2) + eps) * weight (1 without one),
+ * and y into out as fobq_fp8_quantize would (of y in fp32; nothing is rounded to 16 bits on the way).  A row whose mean(s^2) + eps is 0 is 0; one that
+ * holds an Inf or NaN, or whose sums pass fp32, is NaN throughout.  Everything is device memory; row strides in elements.
+ * sum and norm may be X or residual (with its stride); otherwise what is written overlaps nothing that is read. */
+typedef struct {
+    const void* X;             /* `type`, rows x cols (those of out); 1 <= cols <= 32768                   */
+    const void* residual;      /* `type`, same shape, or NULL                                             */
+    const void* weight;        /* `weight_type`, cols, or NULL                                            */
+    void*   sum;               /* `type`: s, or NULL                                                      */
+    void*   norm;              /* `type`: y, or NULL                                                      */
+    int64_t x_ld, residual_ld, sum_ld, norm_ld;
+    int32_t type;              /* fobq_float                                                              */
+    int32_t weight_type;       /* `type` or FOBQ_F32                                                      */
+    float   eps;               /* finite, >= 0                                                            */
+    int32_t reserved;          /* must be 0                                                               */
+} fobq_norm;
+/* out: rows_per_scale 1. */
+int fobq_fp8_rms_norm(fobq_ctx* ctx, const fobq_norm* norm, const fobq_fp8_matrix* out);
+
+/* silu(gate) * up into 8-bit blocks, silu(g) = g / (1 + exp(-g)): X (device, `type`, row stride ld elements) has out->rows rows of 2 out->cols
+ * columns, the gates and behind them the ups.  In fp32, then as fobq_fp8_quantize (rows_per_scale 1).  A block with a gate or an up that is not finite, or with a
+ * product that passes fp32, is NaN; where exp(g) is below 2^-126 the result is 0. */
+int fobq_fp8_swiglu(fobq_ctx* ctx, const void* X, int32_t type, int64_t ld, const fobq_fp8_matrix* out);
+
+/* Which experts each token goes to.  Per token, from its logits x (one for each expert):
+ *   p = softmax(x) or 1 / (1 + exp(-x)) (score);  key = p + bias (p without one);
+ *   groups > 1: the experts are that many groups of neighbours, a group counts as the sum of its group_top (1 or 2) largest keys (of one where it has no
+ *     second), and only the top_groups largest groups are chosen from;
+ *   chosen: the top_k experts of largest keys, the largest first; weight = scale * p, or scale * p / (sum of p over the chosen) (renormalize).
+ * Of equal keys or groups the lowest index comes first.  Keys and groups are compared as they are in 64 bits; without a bias, and with group_top 1 or one
+ * group, logits are compared instead (which order as their scores do, also where those are too small for any type).  Weights are computed in fp32.
+ * An expert whose logit or bias is -Inf is never chosen; slots that no expert is left for hold expert -1 and weight 0.  A token with a NaN
+ * among its logits or the bias, with a bias of +Inf, or (softmax) with a logit of +Inf has experts 0 .. top_k - 1 and weights NaN. */
+typedef enum { FOBQ_SOFTMAX = 0, FOBQ_SIGMOID = 1 } fobq_score;
+typedef struct {
+    const void*  logits;       /* device, `type`, tokens x experts, row stride ld elements                */
+    const float* bias;         /* device fp32, experts, or NULL                                           */
+    int64_t tokens, ld;
+    int32_t type;              /* fobq_float                                                              */
+    int32_t experts;           /* 1 .. 1024                                                               */
+    int32_t top_k;             /* 1 .. 32, no more than the experts of top_groups groups                  */
+    int32_t score;             /* fobq_score                                                              */
+    int32_t groups;            /* 1 .. 64, divides experts; 1: none                                       */
+    int32_t top_groups;        /* 1 .. groups                                                             */
+    int32_t group_top;         /* 1 or 2                                                                  */
+    int32_t renormalize;
+    float   scale;             /* finite                                                                  */
+    int32_t reserved;          /* must be 0                                                               */
+} fobq_router;
+
+/* What comes of it, dense device memory.  Pair token * top_k + slot is one row of work for the expert in that slot; the packed rows are the pairs in the order
+ * of their experts, those of an expert in their own order.  Expert e has packed rows starts[e] .. starts[e + 1] - 1; pairs tells the pair of each packed
+ * row and places the packed row of each pair.  Pairs without an expert (-1) have place -1, and pairs is -1 from starts[experts] on. */
+typedef struct {
+    int32_t* chosen;           /* tokens x top_k                                                          */
+    float*   weights;          /* tokens x top_k                                                          */
+    int32_t* starts;           /* experts + 1                                                             */
+    int32_t* pairs;            /* tokens * top_k                                                          */
+    int32_t* places;           /* tokens x top_k                                                          */
+} fobq_routing;
+/* work: at least fobq_route_workspace's bytes (0: may be NULL), 4-byte aligned.  tokens * top_k below 2^29, tokens below 2^26 - 3. */
+int fobq_route(fobq_ctx* ctx, const fobq_router* router, const fobq_routing* out, void* work, int64_t work_bytes);
+int fobq_route_workspace(fobq_ctx* ctx, int64_t tokens, int32_t experts, int64_t* bytes);
+
+/* The weights of all experts: expert e's is a matrix as above (fobq_fp8_matrix) that begins expert_values bytes (a multiple of 16) and expert_scales scales
+ * behind expert e - 1's.  rows, cols, ld, ld_scales, rows_per_scale and format are those of each. */
+typedef struct {
+    void*   values;
+    float*  scales;
+    int64_t rows, cols, ld, ld_scales, expert_values, expert_scales;
+    int32_t experts;           /* 1 .. 1024                                                               */
+    int32_t rows_per_scale;    /* 1 or 128                                                                */
+    int32_t format;            /* fobq_fp8                                                                */
+    int32_t reserved;          /* must be 0                                                               */
+} fobq_fp8_experts;
+
+/* The products of each expert's rows with its weights: Y[p][n] = sum over columns of A's element (a(p), c) times expert e's element (n, c) for the packed
+ * rows p = starts[e] .. starts[e + 1] - 1 of every expert e.  starts and pairs are those of a fobq_routing for `rows` packed rows (device; starts that do not ascend within
+ * 0 .. rows are kept inside that); a(p) = pairs[p] / top_k (A has the tokens' rows; a packed row whose a(p) is no row of A is not
+ * written), or p itself where pairs is NULL (A has the packed rows; A->rows at least `rows`).  Packed rows of no expert are not written.  Y: device, `type`, rows x
+ * B->rows, row stride ld elements.
+ * Precision, formats and scales as fobq_fp8_matmul's, where the form for up to 16 rows is taken if the experts have up to 16 rows on average
+ * (rows <= 16 experts).  The same bits in every run on equal arguments.  A->ld and B->ld below 2^24. */
+int fobq_fp8_expert_matmul(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8_experts* B, const int32_t* starts, const int32_t* pairs, int32_t top_k,
+                           int64_t rows, void* Y, int32_t type, int64_t ld);
+
+/* Back to the tokens: out[t] = base[t] + sum over slots s, in their order, of weights[t][s] * Y[places[t][s]], in fp32, rounded once.  Y: device, `type`, rows x cols,
+ * row stride ld elements; places outside 0 .. rows - 1 add nothing.  weights, places: device, dense, tokens x top_k (1 .. 32).  base (or NULL) and out: device, `type`,
+ * tokens x cols; out may be base (with its stride).  The same bits in every run on equal arguments. */
+int fobq_expert_sum(fobq_ctx* ctx, const void* Y, int32_t type, int64_t rows, int64_t cols, int64_t ld, const float* weights, const int32_t* places,
+                    int64_t tokens, int32_t top_k, const void* base, int64_t base_ld, void* out, int64_t out_ld);
+
 /* ---- stage-level entry points (test and benchmark hooks) ------------------ */
 
 /* Hinv = H^-1 for symmetric positive definite H via H = L L^T, L^-1, L^-T L^-1
@@ -469,9 +566,26 @@ int fobq_debug_offset_tables(int32_t k, int32_t pad, int64_t h, int64_t w, int32
  *                  out: what a call says of such a matrix (fobq_status)
  *   FOBQ_PLAN_KV4_CHECK  in: pages, page_size, heads, head_dim, reserved, n_seqs, rows, max_pages, table_ld, then addresses (not followed) of
  *                  k_codes, v_codes, k_grids, v_grids, table, lengths
- *                  out: what a call says of such a cache and batch (fobq_status) */
+ *                  out: what a call says of such a cache and batch (fobq_status)
+ *   FOBQ_PLAN_ROUTE  in: tokens, experts
+ *                  out: workgroups that have a part of the tokens each, tokens of a part, bytes of work
+ *   FOBQ_PLAN_EXPERTS  in: compute units, packed rows, experts, rows of B, columns, type of the result (fobq_float), rows of B to a scale
+ *                  out: packed rows and rows of B of a tile, workgroups
+ *   FOBQ_PLAN_NORM_CHECK  in: rows, cols, x_ld, residual_ld, sum_ld, norm_ld, type, weight_type, sign of an eps that is wrong (-1: below 0, 1: Inf; 0: 1e-6), then addresses
+ *                  (not followed) of X, residual, weight, sum, norm
+ *                  out: what a call says of such a norm (fobq_status)
+ *   FOBQ_PLAN_ROUTE_CHECK  in: tokens, ld, type, experts, top_k, score, groups, top_groups, group_top, reserved, then addresses (not followed) of logits, bias, chosen,
+ *                  weights, starts, pairs, places
+ *                  out: what a call says of such a router and routing (fobq_status)
+ *   FOBQ_PLAN_EXPERTS_CHECK  in: rows and columns of A, rows, cols, ld, expert_values and expert_scales of B, experts, rows_per_scale, address (not followed) of B's parts
+ *                  and of pairs, top_k, packed rows, type of the result, its row stride
+ *                  out: what a call says of such matrices (fobq_status)
+ *   FOBQ_PLAN_SUM_CHECK  in: type, rows, cols, ld, tokens, top_k, base (an address, not followed), base_ld, out_ld
+ *                  out: what a call says of such a sum (fobq_status) */
 typedef enum { FOBQ_PLAN_PAD = 0, FOBQ_PLAN_ELIMINATE = 1, FOBQ_PLAN_HESSIAN = 2, FOBQ_PLAN_SLABS = 3, FOBQ_PLAN_FP8_MATMUL = 4,
-               FOBQ_PLAN_KV4_ATTENTION = 5, FOBQ_PLAN_KV4_PLACE = 6, FOBQ_PLAN_FP8_CHECK = 7, FOBQ_PLAN_KV4_CHECK = 8 } fobq_plan;
+               FOBQ_PLAN_KV4_ATTENTION = 5, FOBQ_PLAN_KV4_PLACE = 6, FOBQ_PLAN_FP8_CHECK = 7, FOBQ_PLAN_KV4_CHECK = 8,
+               FOBQ_PLAN_ROUTE = 9, FOBQ_PLAN_EXPERTS = 10, FOBQ_PLAN_NORM_CHECK = 11, FOBQ_PLAN_ROUTE_CHECK = 12, FOBQ_PLAN_EXPERTS_CHECK = 13,
+               FOBQ_PLAN_SUM_CHECK = 14 } fobq_plan;
 
 int fobq_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* out, int32_t n_out);
 

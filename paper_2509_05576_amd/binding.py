@@ -46,6 +46,11 @@ _fp8_matrix = struct.Struct("@PPqqqqii").pack
 _kv4_cache = struct.Struct("@PPPPqiiii").pack
 _kv4_batch = struct.Struct("@PPPqqii").pack
 _kv4_query = struct.Struct("@PPPqqqqqiiiifi").pack
+# and of a feed-forward part of experts: fobq_norm, fobq_router, fobq_routing, fobq_fp8_experts
+_norm = struct.Struct("@PPPPPqqqqiifi").pack
+_router = struct.Struct("@PPqqiiiiiiiifi").pack
+_routing = struct.Struct("@PPPPP").pack
+_fp8_experts = struct.Struct("@PPqqqqqqiiii").pack
 
 
 class FobqLayer(ctypes.Structure):
@@ -99,6 +104,12 @@ def load_library() -> ctypes.CDLL:
     lib.fobq_kv4_read.argtypes = lib.fobq_kv4_append.argtypes
     lib.fobq_kv4_attention.argtypes = [vp, vp, vp, vp, vp, i64]
     lib.fobq_kv4_attention_workspace.argtypes = [vp, vp, vp, vp, ptr(i64)]
+    lib.fobq_fp8_rms_norm.argtypes = [vp, vp, vp]
+    lib.fobq_fp8_swiglu.argtypes = [vp, vp, i32, i64, vp]
+    lib.fobq_route.argtypes = [vp, vp, vp, vp, i64]
+    lib.fobq_route_workspace.argtypes = [vp, i64, i32, ptr(i64)]
+    lib.fobq_fp8_expert_matmul.argtypes = [vp, vp, vp, vp, vp, i32, i64, vp, i32, i64]
+    lib.fobq_expert_sum.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp, i64]
     lib.fobq_probe_int8_matrix_rate.argtypes = [vp, i32, ctypes.POINTER(dbl)]
     lib.fobq_profile_enable.argtypes = [vp, i32]
     lib.fobq_profile_get.argtypes = [vp, i32, ctypes.POINTER(dbl), ctypes.POINTER(i64)]
@@ -109,6 +120,7 @@ def load_library() -> ctypes.CDLL:
                  "fobq_sensitivity_static", "fobq_debug_fail_after", "fobq_debug_wait_looks", "fobq_debug_plan", "fobq_debug_offset_tables", "fobq_workspace_bytes", "fobq_probe_int8_matrix_rate", "fobq_obq_rows", "fobq_hessian_form",
                  "fobq_fp8_quantize", "fobq_fp8_from_codes", "fobq_fp8_matmul", "fobq_fp8_matmul_workspace",
                  "fobq_kv4_append", "fobq_kv4_read", "fobq_kv4_attention", "fobq_kv4_attention_workspace",
+                 "fobq_fp8_rms_norm", "fobq_fp8_swiglu", "fobq_route", "fobq_route_workspace", "fobq_fp8_expert_matmul", "fobq_expert_sum",
                  "fobq_profile_enable", "fobq_profile_get", "fobq_profile_reset"):
         getattr(lib, name).restype = i32
     _lib = lib
@@ -375,6 +387,7 @@ def fobq_debug_wait_looks(ctx: int, looks: int) -> None:
 
 PLAN_PAD, PLAN_ELIMINATE, PLAN_HESSIAN, PLAN_SLABS = 0, 1, 2, 3
 PLAN_FP8_MATMUL, PLAN_KV4_ATTENTION, PLAN_KV4_PLACE, PLAN_FP8_CHECK, PLAN_KV4_CHECK = 4, 5, 6, 7, 8
+PLAN_ROUTE, PLAN_EXPERTS, PLAN_NORM_CHECK, PLAN_ROUTE_CHECK, PLAN_EXPERTS_CHECK, PLAN_SUM_CHECK = 9, 10, 11, 12, 13, 14
 
 
 def fobq_debug_plan(what: int, args, n_out: int):
@@ -679,6 +692,192 @@ def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tens
     return out
 
 
+# ---- a feed-forward part of experts ----------------------------------------------------------------
+def fobq_fp8_rms_norm(ctx: int, x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
+                      format: torch.dtype = torch.float8_e4m3fn, out: Optional[Fp8Matrix] = None, sum: Optional[torch.Tensor] = None,
+                      norm: Optional[torch.Tensor] = None):
+    """x (fp32, bf16 or fp16, rows x cols) + residual, and its root-mean-square norm times weight (cols, x's type or fp32) in 8-bit blocks: (Fp8Matrix, sum).  sum:
+    x + residual, new, or into the tensor given (which may be x or residual); None without a residual if none is given.  norm: filled with the
+    norm in x's type, if given.  No gradient passes it."""
+    _need(x, ctx, _FLOAT, 2, "x")
+    rows, cols = x.shape
+    dtype, device = x.dtype, x.device
+    if weight is not None and (_need(weight, ctx, (dtype, torch.float32), 1, "weight").shape[0] != cols):
+        raise TypeError(f"weight: need {cols} entries, got {weight.shape[0]}")
+    if residual is not None and sum is None:
+        sum = _empty(ctx, (rows, cols), dtype, device)
+    lds = []
+    for name, t in (("residual", residual), ("sum", sum), ("norm", norm)):
+        if t is None:
+            lds.append(cols)
+            continue
+        if _need(t, ctx, (dtype,), 2, name).shape != x.shape:
+            raise TypeError(f"{name}: need {rows} x {cols}, got {tuple(t.shape)}")
+        lds.append(t.stride()[0] if rows > 1 else cols)
+    out, m = _out_fp8(ctx, out, rows, cols, format, 1, device)
+    n = _norm(x.data_ptr(), residual.data_ptr() if residual is not None else 0, weight.data_ptr() if weight is not None else 0,
+              sum.data_ptr() if sum is not None else 0, norm.data_ptr() if norm is not None else 0, x.stride()[0] if rows > 1 else cols, *lds,
+              _FLOAT[dtype], _FLOAT[weight.dtype] if weight is not None else _FLOAT[dtype], eps, 0)
+    _check(ctx, load_library().fobq_fp8_rms_norm(ctx, n, m))
+    return out, sum
+
+
+def fobq_fp8_swiglu(ctx: int, x: torch.Tensor, format: torch.dtype = torch.float8_e4m3fn, out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+    """x (fp32, bf16 or fp16, rows x 2 cols: the gates, then the ups) -> silu(gate) * up, rows x cols, as an Fp8Matrix.  No gradient passes it."""
+    _need(x, ctx, _FLOAT, 2, "x")
+    rows, both = x.shape
+    if both % 2:
+        raise TypeError(f"x: need an even number of columns, got {both}")
+    out, m = _out_fp8(ctx, out, rows, both // 2, format, 1, x.device)
+    _check(ctx, load_library().fobq_fp8_swiglu(ctx, x.data_ptr(), _FLOAT[x.dtype], x.stride()[0] if rows > 1 else both, m))
+    return out
+
+
+@dataclass
+class Routing:
+    """Which experts each token goes to (chosen, int32, tokens x top_k; -1: none) with which weights (fp32), and where the rows of each lie: expert e has packed
+    rows starts[e] .. starts[e + 1] - 1 (int32, experts + 1); pairs (int32, tokens * top_k): the pair token * top_k + slot of each packed row, -1 behind the
+    last expert's; places (int32, tokens x top_k): the packed row of each pair, or -1."""
+    chosen: torch.Tensor
+    weights: torch.Tensor
+    starts: torch.Tensor
+    pairs: torch.Tensor
+    places: torch.Tensor
+
+    @staticmethod
+    def empty(tokens: int, experts: int, top_k: int, device="cuda") -> "Routing":
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)  # noqa: E731
+        return Routing(i32(tokens, top_k), torch.empty((tokens, top_k), device=device), i32(experts + 1), i32(tokens * top_k), i32(tokens, top_k))
+
+
+_SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _dense(t: torch.Tensor, ctx: int, dtype: torch.dtype, shape, what: str) -> int:
+    """The address of a contiguous device tensor of this type and shape."""
+    home = _streams.get(ctx)
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous() and home is not None and t.get_device() == home[0]):
+        got = f"{tuple(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise TypeError(f"{what}: need a contiguous {tuple(shape)} of {dtype} on the context's device, got {got}")
+    return t.data_ptr()
+
+
+def fobq_route(ctx: int, logits: torch.Tensor, top_k: int, *, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1, top_groups: int = 1,
+               group_top: int = 2, renormalize: bool = True, scale: float = 1.0, out: Optional[Routing] = None) -> Routing:
+    """logits (fp32, bf16 or fp16, tokens x experts) -> the top_k experts of each token and their weights.  score: "softmax" or "sigmoid"; bias (fp32, experts): added for
+    the choice, not for the weights; groups: only the top_groups groups of neighbouring experts are chosen from, which count as the sum of their group_top
+    (1 or 2) best; renormalize: the weights are relative to the sum of the chosen ones; scale: times the weights.  No gradient passes it."""
+    _need(logits, ctx, _FLOAT, 2, "logits")
+    tokens, experts = logits.shape
+    if score not in _SCORES:
+        raise TypeError(f"score must be softmax or sigmoid, got {score}")
+    if not (isinstance(top_k, int) and 1 <= top_k <= min(32, experts)):
+        raise TypeError(f"top_k must be in 1..{min(32, experts)}, got {top_k}")
+    i32, f32, device = torch.int32, torch.float32, logits.device
+    if out is None:
+        out = Routing(_empty(ctx, (tokens, top_k), i32, device), _empty(ctx, (tokens, top_k), f32, device), _empty(ctx, (experts + 1,), i32, device),
+                      _empty(ctx, (tokens * top_k,), i32, device), _empty(ctx, (tokens, top_k), i32, device))
+        to = _routing(out.chosen.data_ptr(), out.weights.data_ptr(), out.starts.data_ptr(), out.pairs.data_ptr(), out.places.data_ptr())
+    else:
+        to = _routing(_dense(out.chosen, ctx, i32, (tokens, top_k), "chosen"), _dense(out.weights, ctx, f32, (tokens, top_k), "weights"),
+                      _dense(out.starts, ctx, i32, (experts + 1,), "starts"), _dense(out.pairs, ctx, i32, (tokens * top_k,), "pairs"),
+                      _dense(out.places, ctx, i32, (tokens, top_k), "places"))
+    r = _router(logits.data_ptr(), _dense(bias, ctx, f32, (experts,), "bias") if bias is not None else 0, tokens, logits.stride()[0] if tokens > 1 else experts,
+                _FLOAT[logits.dtype], experts, top_k, _SCORES[score], groups, top_groups, group_top, 1 if renormalize else 0, scale, 0)
+    lib, need = load_library(), ctypes.c_int64(0)
+    _check(ctx, lib.fobq_route_workspace(ctx, tokens, experts, ctypes.byref(need)))
+    work = _scratch(ctx, need.value, device)
+    _check(ctx, lib.fobq_route(ctx, r, to, work.data_ptr() if work is not None else None, need.value))
+    return out
+
+
+@dataclass
+class Fp8Experts:
+    """The weights of all experts: values (float8_e4m3fn or float8_e5m2, experts x rows x cols, rows a multiple of 16 bytes apart) and scales (fp32, experts x
+    ceil(cols / 128) x ceil(rows / rows_per_scale)).  expert(e) is one of them as an Fp8Matrix, for example for fp8_quantize's out."""
+    values: torch.Tensor
+    scales: torch.Tensor
+    rows_per_scale: int = 1
+
+    @staticmethod
+    def empty(experts: int, rows: int, cols: int, format: torch.dtype = torch.float8_e4m3fn, rows_per_scale: int = 128, device="cuda") -> "Fp8Experts":
+        values = torch.empty((experts, rows, (cols + 15) & -16), dtype=format, device=device)[:, :, :cols]
+        return Fp8Experts(values, torch.empty((experts, (cols + 127) // 128, (rows + rows_per_scale - 1) // rows_per_scale), device=device), rows_per_scale)
+
+    def expert(self, e: int) -> Fp8Matrix:
+        return Fp8Matrix(self.values[e], self.scales[e], self.rows_per_scale)
+
+
+def _experts(ctx: int, b: Fp8Experts):
+    """What the library calls the weights of all experts, and how many there are, their rows and columns."""
+    v, s, per = b.values, b.scales, b.rows_per_scale
+    _need(v, ctx, _FP8, 3, "experts.values")
+    _need(s, ctx, _F32, 3, "experts.scales")
+    (count, rows, cols), (apart, ld, _), (scales_apart, ld_scales, _) = v.shape, v.stride(), s.stride()
+    if per not in (1, 128) or s.shape != (count, (cols + 127) // 128, (rows + per - 1) // per):
+        raise TypeError(f"experts: rows_per_scale must be 1 or 128 and scales (experts, ceil(cols / 128), ceil(rows / rows_per_scale)), got {per} and "
+                        f"{tuple(s.shape)} for {tuple(v.shape)}")
+    wide, sr = (cols + 15) & -16, s.shape[2]
+    if rows <= 1 or not cols:
+        ld = wide
+    if count <= 1 or not rows or not cols:
+        apart, scales_apart = 0, 0
+    if wide != cols and count and rows and v.storage_offset() + (count - 1) * apart + (rows - 1) * ld + wide > v.untyped_storage().nbytes():
+        raise TypeError("experts: the last row must be readable to a multiple of 16 bytes")
+    return (_fp8_experts(v.data_ptr(), s.data_ptr(), rows, cols, ld, ld_scales if s.shape[1] > 1 else sr, apart, scales_apart, count, per, _FP8[v.dtype], 0),
+            count, rows, cols)
+
+
+def fobq_fp8_expert_matmul(ctx: int, A: Fp8Matrix, experts: Fp8Experts, routing: Routing, dtype: torch.dtype = torch.bfloat16, *, packed: bool = False,
+                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The packed rows of a routing times their experts' weights transposed -> packed rows x rows of an expert, of `dtype` (fp32, bf16 or fp16), or into `out`.  A:
+    the tokens' rows, or (packed) the packed rows themselves.  Packed rows of no expert are not written (uninitialized in a new result).  Precision as
+    fp8_matmul's, the form for up to 16 rows where the experts have up to 16 on average.  No gradient passes it."""
+    a, m, k = _fp8(ctx, A, "A")
+    b, count, n, k2 = _experts(ctx, experts)
+    if k != k2:
+        raise TypeError(f"A has {k} columns, the experts {k2}")
+    pairs, places = routing.pairs, routing.places
+    if places.dim() != 2 or pairs.dim() != 1 or places.numel() != pairs.shape[0]:
+        raise TypeError(f"routing: need places tokens x top_k and as many pairs, got {tuple(places.shape)} and {tuple(pairs.shape)}")
+    (tokens, top_k), rows = places.shape, pairs.shape[0]
+    if m != (rows if packed else tokens):
+        raise TypeError(f"A has {m} rows, need {rows if packed else tokens}: the {'packed' if packed else 'tokens'}' rows")
+    starts, device = _dense(routing.starts, ctx, torch.int32, (count + 1,), "starts"), A.values.device
+    if out is None:
+        if dtype not in _FLOAT:
+            raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+        out = _empty(ctx, (rows, n), dtype, device)
+    else:
+        _need(out, ctx, _FLOAT, 2, "out")
+        if tuple(out.shape) != (rows, n):
+            raise TypeError(f"out: need {rows} x {n}, got {tuple(out.shape)}")
+        dtype = out.dtype
+    _check(ctx, load_library().fobq_fp8_expert_matmul(ctx, a, b, starts, None if packed else _dense(pairs, ctx, torch.int32, (rows,), "pairs"), max(1, top_k), rows,
+                                                      out.data_ptr(), _FLOAT[dtype], out.stride()[0] if rows > 1 else n))
+    return out
+
+
+def fobq_expert_sum(ctx: int, y: torch.Tensor, routing: Routing, base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y (fp32, bf16 or fp16, packed rows x cols) -> for each token base (tokens x cols, if given) + the sum over its slots of weight times row, in slot order, of y's type;
+    or into `out`, which may be base.  No gradient passes it."""
+    _need(y, ctx, _FLOAT, 2, "y")
+    (rows, cols), dtype = y.shape, y.dtype
+    if routing.places.dim() != 2:
+        raise TypeError(f"places: need tokens x top_k, got {tuple(routing.places.shape)}")
+    tokens, top_k = routing.places.shape
+    places, weights = _dense(routing.places, ctx, torch.int32, (tokens, top_k), "places"), _dense(routing.weights, ctx, torch.float32, (tokens, top_k), "weights")
+    if out is None:
+        out = _empty(ctx, (tokens, cols), dtype, y.device)
+    for name, t in (("out", out), ("base", base)):
+        if t is not None and _need(t, ctx, (dtype,), 2, name).shape != (tokens, cols):
+            raise TypeError(f"{name}: need {tokens} x {cols}, got {tuple(t.shape)}")
+    _check(ctx, load_library().fobq_expert_sum(ctx, y.data_ptr(), _FLOAT[dtype], rows, cols, y.stride()[0] if rows > 1 else cols, weights, places, tokens, top_k,
+                                               base.data_ptr() if base is not None else None, base.stride()[0] if base is not None and tokens > 1 else cols,
+                                               out.data_ptr(), out.stride()[0] if tokens > 1 else cols))
+    return out
+
+
 def FOBQ_PROFILE_STAGE(stage: int) -> int:
     return 2 << stage
 
@@ -769,6 +968,21 @@ class Ctx:
 
     def kv4_attention(self, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tensor, **kw) -> torch.Tensor:
         return fobq_kv4_attention(self.handle, cache, batch, q, **kw)
+
+    def fp8_rms_norm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, **kw):
+        return fobq_fp8_rms_norm(self.handle, x, weight, residual, **kw)
+
+    def fp8_swiglu(self, x: torch.Tensor, format: torch.dtype = torch.float8_e4m3fn, out: Optional[Fp8Matrix] = None) -> Fp8Matrix:
+        return fobq_fp8_swiglu(self.handle, x, format, out)
+
+    def route(self, logits: torch.Tensor, top_k: int, **kw) -> Routing:
+        return fobq_route(self.handle, logits, top_k, **kw)
+
+    def fp8_expert_matmul(self, A: Fp8Matrix, experts: Fp8Experts, routing: Routing, dtype: torch.dtype = torch.bfloat16, **kw) -> torch.Tensor:
+        return fobq_fp8_expert_matmul(self.handle, A, experts, routing, dtype, **kw)
+
+    def expert_sum(self, y: torch.Tensor, routing: Routing, base: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return fobq_expert_sum(self.handle, y, routing, base, out)
 
     def workspace_bytes(self) -> int:
         return fobq_workspace_bytes(self.handle)

@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfobq.so")
 SOURCES = ["api.hip", "gemm64.hip", "hessian.hip", "hessian_i8.hip", "hessian_offsets.hip", "factor.hip", "flow.hip", "quant.hip", "obq.hip", "probe.hip",
-           "api_lowbit.hip", "fp8.hip", "fp8_matmul.hip", "kv4.hip", "kv4_attention.hip"]
+           "api_lowbit.hip", "fp8.hip", "fp8_matmul.hip", "kv4.hip", "kv4_attention.hip",
+           "api_experts.hip", "fp8_norm.hip", "route.hip", "fp8_experts.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-fno-gpu-rdc",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,23 +1,12 @@
 // C ABI of the calls that run a quantized network: argument checks and launches.  They allocate nothing and wait for nothing.
+#include "api_lowbit.h"
 #include "kv4.h"
 
 #include <algorithm>
 
 namespace fobq {
 
-constexpr int64_t MAX_SIDE = (int64_t)1 << 29;      // rows and columns of a matrix, rows times query heads: products with 4 stay in 32 bits
-// A launch has fewer than 2^32 threads: a wavefront for each row of the cache, or for 512 columns of a matrix's row; 256 for a tile.
-constexpr int64_t MAX_ROWS = ((int64_t)1 << 26) - 4, MAX_TILES = ((int64_t)1 << 24) - 1;
-constexpr int64_t MAX_APART = (int64_t)1 << 24;     // rows of a product's matrices: 256 of them stay within 32-bit offsets
-
-static int enter(fobq_ctx* ctx, const DeviceGuard& g) { return g.ok ? FOBQ_OK : set_err(ctx, FOBQ_EHIP, "cannot select device %d", ctx->device); }
-
-static bool aligned(const void* p, int to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-
-static int float_size(int type) { return type == FOBQ_F32 ? 4 : 2; }
-static bool is_float(int type) { return type == FOBQ_F32 || type == FOBQ_BF16 || type == FOBQ_F16; }
-
-static int check_matrix(fobq_ctx* ctx, const fobq_fp8_matrix* m, const char* name, Fp8View* v)
+int check_matrix(fobq_ctx* ctx, const fobq_fp8_matrix* m, const char* name, Fp8View* v)
 {
     if (!m) return set_err(ctx, FOBQ_EINVAL, "%s is NULL", name);
     if (m->rows < 0 || m->rows >= MAX_SIDE || m->cols < 0 || m->cols >= MAX_SIDE)
@@ -138,7 +127,7 @@ int lowbit_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* ou
         out[0] = check_kv4(nullptr, &c, &b, &cv, &sv);
         return FOBQ_OK;
     }
-    return FOBQ_EINVAL;
+    return experts_debug_plan(what, in, n_in, out, n_out);
 }
 
 }  // namespace fobq

@@ -40,6 +40,40 @@ Fp8Plan fp8_matmul_plan(int cus, int64_t m, int64_t n, int64_t k, int type, int 
 int64_t fp8_matmul_workspace(const Fp8Plan& p, int64_t m, int64_t n);
 hipError_t launch_fp8_matmul(hipStream_t s, const Fp8Plan& p, const Fp8View& a, const Fp8View& b, void* y, int type, int64_t ldy, float* work);
 
+// what a norm reads and writes beside its 8-bit blocks (fobq_norm, checked)
+struct NormView { const void *x, *residual, *weight; void *sum, *norm; int64_t x_ld, residual_ld, sum_ld, norm_ld; float eps; Fp8View out; };
+hipError_t launch_rms_norm(hipStream_t s, const NormView& g, int type, int weight_type);
+hipError_t launch_swiglu(hipStream_t s, const void* x, int type, int64_t ld, const Fp8View& out);
+
+// A router's call (fobq_router, fobq_routing, checked).  parts: workgroups that each have `per_part` tokens (a multiple of 64) in a row; more than one of them
+// count their tokens' experts into `work` (parts x experts), and a second launch has the places.
+struct RoutePlan { int parts, per_part; };
+RoutePlan route_plan(int64_t tokens);
+int64_t route_workspace(const RoutePlan& p, int experts);
+struct RouteView {
+    const void* logits; const float* bias; int64_t ld;
+    int tokens, experts, top, score, groups, top_groups, group_top, renormalize; float scale;
+    int32_t* chosen; float* weights; int32_t *starts, *pairs, *places;
+};
+hipError_t launch_route(hipStream_t s, const RoutePlan& p, const RouteView& g, int type, int32_t* work);
+
+// The products of experts' rows: b is expert 0's matrix, the others lie behind it.  tm, tn: packed rows and rows of B to a workgroup; tiles: workgroups
+// that all tiles fit in, however the packed rows are dealt among the experts.
+struct ExpertView {
+    Fp8View a, b; int experts; int64_t expert_values, expert_scales;
+    const int32_t *starts, *pairs; int top, rows;
+    void* y; int type; int64_t ldy;
+};
+struct ExpertPlan { int tm, tn; int64_t tiles; };
+ExpertPlan expert_plan(int cus, int64_t rows, int experts, int64_t n, int64_t k, int type, int per);
+hipError_t launch_expert_matmul(hipStream_t s, const ExpertPlan& p, const ExpertView& g);
+
+struct ExpertSum {
+    const void* y; int64_t ld; int rows; const float* weights; const int32_t* places; int tokens, top; int64_t cols;
+    const void* base; int64_t base_ld; void* out; int64_t out_ld;
+};
+hipError_t launch_expert_sum(hipStream_t s, const ExpertSum& g, int type);
+
 // the cache and the sequences of a call (fobq_kv4_cache, fobq_kv4_batch, checked); a page has 1 << shift tokens
 struct Kv4View { uint8_t *k_codes, *v_codes; uint32_t *k_grids, *v_grids; int pages, heads, dim, shift; };
 struct Kv4Seqs { const int32_t *table, *lengths, *starts; int64_t table_ld; int n_seqs, max_pages, rows; };

@@ -1,0 +1,158 @@
+"""The norm and the gated activation into 8-bit blocks on the GPU, against 64-bit forms."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import experts_reference as ref
+from lowbit_reference import HALF, U
+
+pytestmark = pytest.mark.gpu
+E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
+F32, BF, HF = torch.float32, torch.bfloat16, torch.float16
+SIZES = [(1, 1), (3, 127), (2, 128), (5, 129), (4, 1000), (7, 1024), (3, 1025), (300, 96), (9, 4608), (2, 16384), (2, 16385), (1, 32768)]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_2509_05576_amd as fobq
+    c = fobq.Ctx(0)
+    yield c
+    c.close()
+
+
+def _x(rows, cols, dtype, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn((rows, cols), generator=g) * torch.exp(spread * torch.randn((rows, 1), generator=g))).to(dtype)
+
+
+def _near(got, want, err, dtype):
+    """A value that the kernel has in fp32 within err, rounded to dtype."""
+    bound = err + HALF[dtype] * (want.abs() + err) * 1.01 + torch.finfo(dtype).smallest_normal * HALF[dtype]
+    return ((got.cpu().double() - want).abs() <= bound).all()
+
+
+def check_norm(m, total, plain, x, weight, residual, eps, fmt):
+    s, y = ref.rms_norm(x, weight, residual, eps)
+    # s rounded (U), the others' roundings in the rms (U), 1 / rms (U), three products
+    ref.check_blocks(m.values, m.scales, y, y.abs() * 6.1 * U, fmt)
+    if total is not None:
+        assert _near(total, s, s.abs() * U, x.dtype)
+    if plain is not None:
+        assert _near(plain, y, y.abs() * 6.1 * U, x.dtype)
+
+
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("dtype,wtype", [(F32, F32), (BF, BF), (BF, F32), (HF, HF), (HF, F32)])
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_norm(ctx, rows, cols, dtype, wtype, fmt):
+    x, r = _x(rows, cols, dtype, cols), _x(rows, cols, dtype, cols + 1)
+    w = (1 + 0.3 * _x(1, cols, F32, 5, 0.0)[0]).to(wtype)
+    plain = torch.full((rows, cols), 7.0, dtype=dtype, device="cuda")
+    m, total = ctx.fp8_rms_norm(x.cuda(), w.cuda(), r.cuda(), eps=1e-5, format=fmt, norm=plain)
+    assert m.values.dtype == fmt and m.values.shape == x.shape and m.values.stride(0) % 16 == 0 and total.dtype == dtype
+    check_norm(m, total, plain, x, w, r, 1e-5, fmt)
+    # without a residual, without a weight
+    m, none = ctx.fp8_rms_norm(x.cuda(), eps=1e-5, format=fmt)
+    assert none is None
+    check_norm(m, None, None, x, None, None, 1e-5, fmt)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+@pytest.mark.parametrize("into", ["x", "residual"])
+def test_norm_in_place_and_strides(ctx, dtype, into):
+    """Rows of wider matrices that begin anywhere, the sum written over one of them; the columns beside are left alone."""
+    rows, cols = 37, 1111
+    wide = [torch.cat((_x(rows, 3, dtype, 1), _x(rows, cols, dtype, 2 + i), _x(rows, 7, dtype, 9)), 1) for i in range(2)]
+    there = [t.cuda() for t in wide]
+    x, r = (t[:, 3:3 + cols] for t in there)
+    s = x if into == "x" else r
+    m, total = ctx.fp8_rms_norm(x, None, r, sum=s)
+    assert total is s
+    check_norm(m, s, None, wide[0][:, 3:3 + cols], None, wide[1][:, 3:3 + cols], 1e-6, E4)
+    for i, t in enumerate(there):
+        if (i == 0) == (into == "x"):
+            assert torch.equal(t[:, :3].cpu(), wide[i][:, :3]) and torch.equal(t[:, 3 + cols:].cpu(), wide[i][:, 3 + cols:])
+        else:
+            assert torch.equal(t.cpu(), wide[i])
+
+
+def test_norm_into_a_given_matrix(ctx):
+    import paper_2509_05576_amd as fobq
+    x = _x(5, 200, BF, 3).cuda()
+    want, _ = ctx.fp8_rms_norm(x)
+    values = torch.full((5, 256), 3, dtype=torch.uint8, device="cuda")
+    out = fobq.Fp8Matrix(values.view(E4)[:, :200], torch.full((2, 9), -5.0, device="cuda")[:, :5], 1)
+    got, _ = ctx.fp8_rms_norm(x, out=out)
+    assert got is out and torch.equal(out.values.view(torch.uint8), want.values.view(torch.uint8)) and torch.equal(out.scales, want.scales)
+    assert bool((values[:, 200:] == 3).all())
+
+
+def test_norm_extremes(ctx):
+    """Rows of the largest and of the smallest values, of zeros, and such that are not finite: each row by itself."""
+    x = _x(9, 1500, F32, 4, 0.0)
+    x[1] *= 1e38
+    x[1].clamp_(-3e38, 3e38)
+    x[2] *= 1e-38
+    x[3] = 0
+    x[4, 1400] = math.inf
+    x[5, 3] = math.nan
+    x[6, 0] = 3e38                                         # beside it all others are nothing
+    x[7] *= 2.0 ** -140
+    for eps in (0.0, 1e-6):
+        plain = torch.empty_like(x, device="cuda")
+        m, _ = ctx.fp8_rms_norm(x.cuda(), None, None, eps=eps, norm=plain)
+        s, y = ref.rms_norm(x, None, None, float(torch.tensor(eps)))
+        # (rows of denormal values: y = s * pre is exact, or, where pre is at its most, still within the bound)
+        ref.check_blocks(m.values, m.scales, y, y.abs() * 6.1 * U + 2.0 ** -149, E4)
+        assert bool(plain[4:6].isnan().all()) and bool(plain[[0, 1, 2, 3, 6, 7, 8]].isfinite().all())
+    big = torch.full((1, 256), 2e38)
+    m, total = ctx.fp8_rms_norm(big.cuda(), None, big.cuda())   # the addition passes fp32
+    assert bool(total.isinf().all()) and bool(m.scales.isnan().all()) and bool(m.values.float().isnan().all())
+
+
+def test_norm_refusals(ctx):
+    import paper_2509_05576_amd as fobq
+    x = torch.zeros((4, 256), dtype=BF, device="cuda")
+    for bad in (lambda: ctx.fp8_rms_norm(x.cpu()), lambda: ctx.fp8_rms_norm(x.t()), lambda: ctx.fp8_rms_norm(x.int()), lambda: ctx.fp8_rms_norm(x, x[0, :5]),
+                lambda: ctx.fp8_rms_norm(x, x[0].half()), lambda: ctx.fp8_rms_norm(x, None, x[:3]), lambda: ctx.fp8_rms_norm(x, None, x.float()),
+                lambda: ctx.fp8_rms_norm(x, format=BF), lambda: ctx.fp8_rms_norm(x, norm=x[:, :5]), lambda: ctx.fp8_rms_norm(x, sum=x.float()),
+                lambda: ctx.fp8_rms_norm(x, out=ctx.fp8_quantize(x[:3])), lambda: ctx.fp8_swiglu(x[:, :5]), lambda: ctx.fp8_swiglu(x.int()),
+                lambda: ctx.fp8_swiglu(x, out=ctx.fp8_quantize(x))):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: ctx.fp8_rms_norm(x, eps=-1.0), lambda: ctx.fp8_rms_norm(x, eps=math.inf), lambda: ctx.fp8_rms_norm(x, eps=math.nan),
+                lambda: ctx.fp8_rms_norm(x[:, :0]), lambda: ctx.fp8_rms_norm(torch.zeros((1, 32769), device="cuda")),
+                lambda: ctx.fp8_rms_norm(x, out=ctx.fp8_quantize(x, rows_per_scale=128)),
+                lambda: ctx.fp8_swiglu(x, out=ctx.fp8_quantize(x[:, :128], rows_per_scale=128))):
+        with pytest.raises(fobq.FobqError):
+            bad()
+    m, _ = ctx.fp8_rms_norm(x[:0])
+    assert m.values.shape == (0, 256) and ctx.fp8_swiglu(x[:0]).values.shape == (0, 128) and ctx.fp8_swiglu(x[:, :0]).values.shape == (4, 0)
+
+
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_swiglu(ctx, rows, cols, dtype, fmt):
+    x = _x(rows, 2 * cols, dtype, cols, 1.5)
+    m = ctx.fp8_swiglu(x.cuda(), fmt)
+    y, rel, tiny = ref.swiglu(x)
+    ref.check_blocks(m.values, m.scales, y, y.abs() * rel + tiny, fmt)
+
+
+def test_swiglu_extremes(ctx):
+    """Gates far to either side, products at the ends of fp32 and values that are not finite: each block of 128 by itself."""
+    cols = 128 * 8
+    g, u = _x(3, cols, F32, 1, 0.0), _x(3, cols, F32, 2, 0.0)
+    g[:, 128:256] = torch.linspace(-120, 120, 128)
+    u[:, 256:384] = 1e30
+    g[:, 256:384] = torch.linspace(-95, -60, 128)
+    g[0, 384], u[1, 512], g[2, 640] = math.nan, math.inf, -math.inf
+    g[:, 768:896], u[:, 768:896] = 1e25, 1e25             # passes fp32
+    wide = torch.cat((torch.zeros(3, 5), g, u, torch.zeros(3, 3)), 1).cuda()
+    m = ctx.fp8_swiglu(wide[:, 5:5 + 2 * cols])
+    y, rel, tiny = ref.swiglu(torch.cat((g, u), 1))
+    y[:, 768:896] = math.inf
+    y[~torch.isfinite(g)] = math.nan
+    ref.check_blocks(m.values, m.scales, y, (y.abs() * rel + tiny).nan_to_num(0.0, 0.0, 0.0), E4)
