@@ -454,8 +454,9 @@ typedef struct {
  * 0 .. rows are kept inside that); a(p) = pairs[p] / top_k (A has the tokens' rows; a packed row whose a(p) is no row of A is not
  * written), or p itself where pairs is NULL (A has the packed rows; A->rows at least `rows`).  Packed rows of no expert are not written.  Y: device, `type`, rows x
  * B->rows, row stride ld elements.
- * Precision, formats and scales as fobq_fp8_matmul's, where the form for up to 16 rows is taken if the experts have up to 16 rows on average
- * (rows <= 16 experts).  The same bits in every run on equal arguments.  A->ld and B->ld below 2^24. */
+ * Formats, scales and precision as fobq_fp8_matmul's: F32 sums in fp32; 16-bit types as it does for more than 16 rows, but in fp32 where the experts have up to 8
+ * rows on average and the call does not fill the device (which its sizes decide, not how the rows are dealt).  The same bits in every run on equal
+ * arguments.  A->ld and B->ld below 2^24. */
 int fobq_fp8_expert_matmul(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8_experts* B, const int32_t* starts, const int32_t* pairs, int32_t top_k,
                            int64_t rows, void* Y, int32_t type, int64_t ld);
 

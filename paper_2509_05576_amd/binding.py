@@ -832,7 +832,7 @@ def fobq_fp8_expert_matmul(ctx: int, A: Fp8Matrix, experts: Fp8Experts, routing:
                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The packed rows of a routing times their experts' weights transposed -> packed rows x rows of an expert, of `dtype` (fp32, bf16 or fp16), or into `out`.  A:
     the tokens' rows, or (packed) the packed rows themselves.  Packed rows of no expert are not written (uninitialized in a new result).  Precision as
-    fp8_matmul's, the form for up to 16 rows where the experts have up to 16 on average.  No gradient passes it."""
+    fp8_matmul's for more than 16 rows, or better.  No gradient passes it."""
     a, m, k = _fp8(ctx, A, "A")
     b, count, n, k2 = _experts(ctx, experts)
     if k != k2:

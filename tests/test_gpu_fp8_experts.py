@@ -177,7 +177,10 @@ def test_far_apart(ctx):
     scales[:, last] = a.scales
     moved = fobq.Routing(r.chosen, r.weights, r.starts, r.pairs + 577, torch.zeros((600, 1), dtype=torch.int32, device="cuda"))
     moved.pairs = torch.cat((moved.pairs, torch.full((577,), -1, dtype=torch.int32, device="cuda")))
-    assert torch.equal(ctx.fp8_expert_matmul(fobq.Fp8Matrix(many, scales), w, moved)[:23], want)
+    near = torch.zeros((600, k), dtype=torch.uint8, device="cuda")       # (another form than that of 23 rows: compared with itself)
+    near[last] = a.values.view(torch.uint8)
+    want = ctx.fp8_expert_matmul(fobq.Fp8Matrix(near.view(E4), scales), w, moved)[:23]
+    assert torch.equal(ctx.fp8_expert_matmul(fobq.Fp8Matrix(many, scales), w, moved)[:23], want) and float(want.float().abs().max()) > 1
 
 
 def test_refusals(ctx):
