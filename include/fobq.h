@@ -433,7 +433,7 @@ typedef struct {
     int32_t* pairs;            /* tokens * top_k                                                          */
     int32_t* places;           /* tokens x top_k                                                          */
 } fobq_routing;
-/* work: at least fobq_route_workspace's bytes (0: may be NULL), 4-byte aligned.  tokens * top_k below 2^29, tokens below 2^26 - 3. */
+/* work: at least fobq_route_workspace's bytes (0: may be NULL), 16-byte aligned.  tokens * top_k below 2^29, tokens below 2^26 - 3. */
 int fobq_route(fobq_ctx* ctx, const fobq_router* router, const fobq_routing* out, void* work, int64_t work_bytes);
 int fobq_route_workspace(fobq_ctx* ctx, int64_t tokens, int32_t experts, int64_t* bytes);
 

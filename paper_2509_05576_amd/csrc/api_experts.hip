@@ -203,8 +203,8 @@ int fobq_route(fobq_ctx* ctx, const fobq_router* router, const fobq_routing* out
     if (rc) return rc;
     const RoutePlan p = route_plan(v.tokens);
     const int64_t need = route_workspace(p, v.experts);
-    if (work_bytes < need || (need > 0 && (!work || !aligned(work, 4))))
-        return set_err(ctx, FOBQ_EINVAL, "work must be %lld bytes, 4-byte aligned (got %lld)", (long long)need, (long long)work_bytes);
+    if (work_bytes < need || (need > 0 && (!work || !aligned(work, 16))))
+        return set_err(ctx, FOBQ_EINVAL, "work must be %lld bytes, 16-byte aligned (got %lld)", (long long)need, (long long)work_bytes);
     DeviceGuard g(ctx->device);
     if ((rc = enter(ctx, g))) return rc;
     FOBQ_TRY(launch_route(ctx->stream, p, v, router->type, need ? static_cast<int32_t*>(work) : nullptr), "routing to experts");

@@ -82,7 +82,7 @@ def test_tokens_are_covered(experts):
     for tokens in (0, 1, 63, 64, 65, 1000, 16384, 16385, 100000, (1 << 26) - 4):
         parts, per, work = fobq.fobq_debug_plan(fobq.PLAN_ROUTE, [tokens, experts], 3)
         assert 1 <= parts <= 256 and per % 64 == 0 and parts * per >= tokens and (parts == 1 or (parts - 1) * per < tokens)
-        assert work == (4 * parts * experts if parts > 1 else 0)
+        assert work == (16 * parts * -(-experts // 4) if parts > 1 else 0)
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
