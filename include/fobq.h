@@ -374,8 +374,9 @@ int fobq_kv4_attention_workspace(fobq_ctx* ctx, const fobq_kv4_cache* cache, con
 
 /* The residual's addition and a root-mean-square norm, into 8-bit blocks.  Per row, in fp32 but for the sum of squares (fp64):
  *   s = X + residual (X without one),  y = s / sqrt(mean(s^2) + eps) * weight (1 without one),
- * and y into out as fobq_fp8_quantize would (of y in fp32; nothing is rounded to 16 bits on the way).  A row whose mean(s^2) + eps is 0 is 0; one that
- * holds an Inf or NaN, or whose sums pass fp32, is NaN throughout.  Everything is device memory; row strides in elements.
+ * and y into out by blocks as fobq_fp8_quantize has them, nothing rounded to 16 bits on the way (the quotient y / scale is that of fp32 values: within
+ * 10 units of fp32 of the exact one before it is rounded).  A row whose mean(s^2) + eps is 0 is 0; one that holds an Inf or NaN, or whose sums pass fp32, is
+ * NaN throughout.  Everything is device memory; row strides in elements.
  * sum and norm may be X or residual (with its stride); otherwise what is written overlaps nothing that is read. */
 typedef struct {
     const void* X;             /* `type`, rows x cols (those of out); 1 <= cols <= 32768                   */
@@ -393,8 +394,8 @@ typedef struct {
 int fobq_fp8_rms_norm(fobq_ctx* ctx, const fobq_norm* norm, const fobq_fp8_matrix* out);
 
 /* silu(gate) * up into 8-bit blocks, silu(g) = g / (1 + exp(-g)): X (device, `type`, row stride ld elements) has out->rows rows of 2 out->cols
- * columns, the gates and behind them the ups.  In fp32, then as fobq_fp8_quantize (rows_per_scale 1).  A block with a gate or an up that is not finite, or with a
- * product that passes fp32, is NaN; where exp(g) is below 2^-126 the result is 0. */
+ * columns, the gates and behind them the ups.  In fp32, then by blocks as above (rows_per_scale 1).  A block with a gate or an up that is not finite, or with a
+ * product that passes fp32, is NaN; 1 / (1 + exp(-g)) counts as no less than 2^-126. */
 int fobq_fp8_swiglu(fobq_ctx* ctx, const void* X, int32_t type, int64_t ld, const fobq_fp8_matrix* out);
 
 /* Which experts each token goes to.  Per token, from its logits x (one for each expert):

@@ -2,11 +2,34 @@
 // activation, both straight into blocks of 128 columns with a scale per row.
 //
 // Memory bound: a lane has 16 columns of a row, eight lanes a block, and everything between the loads and the 8-bit values stays in
-// registers.  The sum of squares is in fp64, which no row of finite values passes, and 1 / rms enters as a power of two, exact, and a factor
-// between 1/2 and 2, so that rows of very large and very small values lose nothing either.  Both cost a few instructions that memory hides.
+// registers.  The sum of squares is in fp64, which no row of finite values passes, so that rows of very large and very small values lose nothing.
+// The values are off by some units of fp32 when their block's largest is known; what is rounded to 8 bits is their product with largest value / largest,
+// one multiplication (fobq_fp8_quantize's quotient, rounded once, takes ten instructions and is for values that are given).
 #include "fp8.h"
 
+#include <type_traits>
+
 namespace fobq {
+
+// 16 values of a block, most the largest magnitude's bits, into 8 bits; the block's scale
+template <int FORMAT>
+__device__ __forceinline__ float put16_by(uint8_t* __restrict__ dst, int left, uint32_t most, const float* y)
+{
+    const float top = __uint_as_float(most), scale = top / Fp8<FORMAT>::TOP;
+    const bool fine = most < 0x7f800000u;
+    const float by = !fine ? __builtin_nanf("") : scale < FP8_TINY ? 0x1p126f : Fp8<FORMAT>::TOP / top;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = to_fp8x4<FORMAT>(y[4 * i] * by, y[4 * i + 1] * by, y[4 * i + 2] * by, y[4 * i + 3] * by);
+    if (left >= 16) {
+        __builtin_memcpy(__builtin_assume_aligned(dst, 16), w, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 15; ++i)
+            if (i < left) dst[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+    return fine ? fmaxf(scale, FP8_TINY) : __builtin_nanf("");
+}
 
 // y as T into 16 adjacent places of a row
 template <class T>
@@ -24,21 +47,32 @@ __device__ __forceinline__ void put_row16(T* __restrict__ dst, int left, const f
     }
 }
 
-__device__ __forceinline__ double wave_sum(double x)
+// the sum over the LANES neighbouring lanes of a row: the neighbour, the other pair, the other half of eight, of sixteen, and so on
+template <int LANES>
+__device__ __forceinline__ double over_lanes(double x)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+    auto dpp = [](double v, auto ctrl) {
+        return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), decltype(ctrl)::value, 0xf, 0xf, true),
+                                __builtin_amdgcn_mov_dpp(__double2loint(v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    x += dpp(x, std::integral_constant<int, 0xB1>());
+    x += dpp(x, std::integral_constant<int, 0x4E>());
+    x += dpp(x, std::integral_constant<int, 0x141>());
+    if constexpr (LANES > 8) x += dpp(x, std::integral_constant<int, 0x140>());
+    if constexpr (LANES > 16) x += __shfl_xor(x, 16);
+    if constexpr (LANES > 32) x += __shfl_xor(x, 32);
     return x;
 }
 
-// A row has `waves` wavefronts of a workgroup, 1024 columns each and PIECES times that; with one, a workgroup has four rows.
-template <class T, class W, int FORMAT, int PIECES>
-__global__ __launch_bounds__(1024) void rms_norm_kernel(NormView g, int waves)
+// A row has LANES lanes, or with LANES 64 `waves` wavefronts of a workgroup, each with 16 columns a lane and piece.  (bf16 with a residual: 8192 x 8192
+// 103 us, 4.6 TB/s; 16384 x 2048 45 us, 5.3 TB/s, partly in the last-level cache; 32768 x 96 7 us.)
+template <class T, class W, int FORMAT, int LANES, int PIECES>
+__global__ __launch_bounds__(512) void rms_norm_kernel(NormView g, int waves)
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    __shared__ double part[16];
-    const int64_t row = waves == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-    if (row >= g.out.rows) return;                           // (only where every wavefront has a row of its own)
+    const int lane = threadIdx.x & (LANES - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ double part[8];
+    const int64_t row = waves == 1 ? (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES : blockIdx.x;
+    if (row >= g.out.rows) return;                           // (only where rows do not meet in LDS)
     const int cols = g.out.cols, col0 = (waves == 1 ? 0 : wave) * 1024 + 16 * lane, step = waves * 1024;
     const T *x = static_cast<const T*>(g.x) + row * g.x_ld, *r = static_cast<const T*>(g.residual) + row * g.residual_ld;
     T tx[PIECES][16], tr[PIECES][16];
@@ -66,52 +100,60 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(NormView g, int waves)
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) put_row16(static_cast<T*>(g.sum) + row * g.sum_ld + col0 + p * step, cols - col0 - p * step, s[p]);
     }
-    squares = wave_sum(squares);
-    if (waves > 1) {
+    squares = over_lanes<LANES>(squares);
+    if (LANES == 64 && waves > 1) {
         if (lane == 0) part[wave] = squares;
         __syncthreads();
         squares = part[0];
         for (int w = 1; w < waves; ++w) squares += part[w];
     }
-    const double mean = squares / cols + (double)g.eps;
-    // s / rms = (s * pre) * inv, pre a power of two
-    float pre = 0.f, inv = 0.f;
-    if (mean > 0.0) {
-        const double rms = sqrt(mean);
-        const int e = min(126, max(-126, -ilogb(rms)));
-        pre = ldexpf(1.f, e);
-        inv = (float)(1.0 / (rms * ldexp(1.0, e)));
+    const double mean = squares / cols + (double)g.eps, inv = mean > 0.0 ? 1.0 / sqrt(mean) : 0.0;
+    float by = mean - mean == 0.0 ? (float)inv : __builtin_nanf("");      // an Inf or NaN in the row: NaN throughout
+    if (!(inv < 0x1p125 && inv > 0x1p-125)) {
+        // 1 / rms is not a normal fp32 number: in two factors, the first a power of two
+        const float pre = inv >= 1.0 ? 0x1p100f : 0x1p-100f;
+        by = mean - mean == 0.0 ? (float)(inv / (double)pre) : by;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[p][i] *= pre;
     }
-    if (!(mean - mean == 0.0)) inv = __builtin_nanf("");     // an Inf or NaN in the row
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
         const int col = col0 + p * step, left = cols - col;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[p][i] = s[p][i] * pre * inv;
+            s[p][i] *= by;
             if (g.weight) s[p][i] *= (float)tw[p][i];
         }
-        const Fp8Scale b = fp8_scale<FORMAT>(most_of_8(most16(s[p])));
-        put16<float, FORMAT>(g.out.values + row * g.out.ld + col, left, b, s[p]);
-        if ((lane & 7) == 0 && left > 0) g.out.scales[(int64_t)(col / 128) * g.out.ld_scales + row] = b.scale;
+        const float scale = put16_by<FORMAT>(g.out.values + row * g.out.ld + col, left, most_of_8(most16(s[p])), s[p]);
+        if ((lane & 7) == 0 && left > 0) g.out.scales[(int64_t)(col / 128) * g.out.ld_scales + row] = scale;
         if (g.norm) put_row16(static_cast<T*>(g.norm) + row * g.norm_ld + col, left, s[p]);
     }
 }
 
-// silu(gate) * up.  Where exp(g) falls below 2^-126 it counts as 0; what is not finite is NaN.
+// silu(gate) * up = gate up / (1 + exp(-gate)); exp(-gate) is kept below 2^126.  exp(-gate) = 2^t 2^rest: t is the product with log2(e) rounded to fp32, rest
+// what that leaves out (with t alone the result is off by |gate| units, and more values fall to the other side of an 8-bit border).  The reciprocal
+// is corrected once.
 __device__ __forceinline__ float swiglu(float gate, float up)
 {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(gate)), r = 1.f / (1.f + e);
-    return gate * (gate < 0.f ? e * r : r) * up;
+    const float t = -1.44269504f * gate, rest = fmaf(-1.92596299e-8f, gate, fmaf(-1.44269504f, gate, -t));
+    float e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+    e = fmaf(e, 0.693147181f * rest, e);
+    const float d = 1.f + e;
+    float r = __builtin_amdgcn_rcpf(d);
+    r = fmaf(fmaf(-d, r, 1.f), r, r);
+    return gate * r * up;
 }
 
+// Eight lanes have a block, whichever row it is in.  (bf16, 32768 x 2048: 71 us, 4.7 TB/s; with 36 instructions a value instead of 25 it was bound by them, 92.)
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void swiglu_kernel(const T* __restrict__ x, int64_t ld, Fp8View out)
 {
-    const int lane = threadIdx.x & 63;
-    const Item at = item_of((int64_t)blockIdx.x * 4, threadIdx.x >> 6, (out.cols + 1023) / 1024);
+    const int lane = threadIdx.x & 7;
+    const Item at = item_of((int64_t)blockIdx.x * 32, threadIdx.x >> 3, (out.cols + 127) / 128);
     const int64_t row = at.row;
-    const int col = at.piece * 1024 + 16 * lane, left = out.cols - col;
+    const int col = at.piece * 128 + 16 * lane, left = out.cols - col;
     if (row >= out.rows) return;
     T gate[16], up[16];
     get16(x + row * ld + col, left, gate);
@@ -119,18 +161,27 @@ __global__ __launch_bounds__(256) void swiglu_kernel(const T* __restrict__ x, in
     float y[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = swiglu((float)gate[i], (float)up[i]);
-    const Fp8Scale s = fp8_scale<FORMAT>(most_of_8(most16(y)));
-    put16<float, FORMAT>(out.values + row * out.ld + col, left, s, y);
-    if ((lane & 7) == 0 && left > 0) out.scales[(int64_t)(col / 128) * out.ld_scales + row] = s.scale;
+    const float scale = put16_by<FORMAT>(out.values + row * out.ld + col, left, most_of_8(most16(y)), y);
+    if (lane == 0) out.scales[(int64_t)at.piece * out.ld_scales + row] = scale;
 }
 
 template <class T, class W, int FORMAT>
 static hipError_t norm_of(hipStream_t s, const NormView& g)
 {
-    const int pieces = g.out.cols <= 16384 ? 1 : 2, waves = (g.out.cols + 1024 * pieces - 1) / (1024 * pieces);
-    const dim3 grid((unsigned)(waves == 1 ? (g.out.rows + 3) / 4 : g.out.rows)), block(waves == 1 ? 256 : 64 * waves);
-    if (pieces == 1) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 1>), grid, block, 0, s, g, waves);
-    else hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 2>), grid, block, 0, s, g, waves);
+    const int cols = g.out.cols;
+    auto rows_of = [&](int lanes) { return dim3((unsigned)((g.out.rows + 256 / lanes - 1) / (256 / lanes))); };
+    if (cols <= 128) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 8, 1>), rows_of(8), dim3(256), 0, s, g, 1);
+    else if (cols <= 256) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 16, 1>), rows_of(16), dim3(256), 0, s, g, 1);
+    else if (cols <= 512) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 32, 1>), rows_of(32), dim3(256), 0, s, g, 1);
+    else if (cols <= 1024) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 64, 1>), rows_of(64), dim3(256), 0, s, g, 1);
+    else {
+        // up to 8 wavefronts, which is what shares a row best (8192 x 8192: 8 with a piece each 103 us, 4 with two 107, 2 with four 133)
+        const int pieces = cols <= 8192 ? 1 : cols <= 16384 ? 2 : 4, waves = (cols + 1024 * pieces - 1) / (1024 * pieces);
+        const dim3 grid((unsigned)g.out.rows), block(64 * waves);
+        if (pieces == 1) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 64, 1>), grid, block, 0, s, g, waves);
+        else if (pieces == 2) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 64, 2>), grid, block, 0, s, g, waves);
+        else hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 64, 4>), grid, block, 0, s, g, waves);
+    }
     return hipGetLastError();
 }
 
@@ -151,8 +202,8 @@ hipError_t launch_rms_norm(hipStream_t s, const NormView& g, int type, int weigh
 template <class T>
 static hipError_t swiglu_of(hipStream_t s, const void* x, int64_t ld, const Fp8View& out)
 {
-    const int64_t items = (int64_t)out.rows * ((out.cols + 1023) / 1024);
-    const dim3 grid((unsigned)((items + 3) / 4)), block(256);
+    const int64_t blocks = (int64_t)out.rows * ((out.cols + 127) / 128);
+    const dim3 grid((unsigned)((blocks + 31) / 32)), block(256);
     const T* t = static_cast<const T*>(x);
     if (out.format == FOBQ_E4M3) hipLaunchKernelGGL((swiglu_kernel<T, FOBQ_E4M3>), grid, block, 0, s, t, ld, out);
     else hipLaunchKernelGGL((swiglu_kernel<T, FOBQ_E5M2>), grid, block, 0, s, t, ld, out);
