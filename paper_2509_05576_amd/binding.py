@@ -693,6 +693,35 @@ def fobq_kv4_attention(ctx: int, cache: Kv4Cache, batch: Kv4Batch, q: torch.Tens
 
 
 # ---- a feed-forward part of experts ----------------------------------------------------------------
+def _new(ctx: int, rows: int, cols: int, dtype: torch.dtype, device) -> torch.Tensor:
+    """_empty for a matrix (with strides given torch takes 1.3 us for it instead of 1.6)."""
+    home = _streams.get(ctx)
+    if home is None or _current_stream(device.index) == home[1]:
+        return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+    return _empty(ctx, (rows, cols), dtype, device)
+
+
+def _new_rows(ctx: int, rows: int, cols: int, format: torch.dtype, device):
+    """_new_fp8 with a scale per row."""
+    if format not in _FP8:
+        raise TypeError(f"format must be float8_e4m3fn or float8_e5m2, got {format}")
+    wide, blocks = (cols + 15) & -16, (cols + 127) // 128
+    values, scales = _new(ctx, rows, wide, format, device), _new(ctx, blocks, rows, torch.float32, device)
+    return (Fp8Matrix(values if wide == cols else values[:, :cols], scales, 1),
+            _fp8_matrix(values.data_ptr(), scales.data_ptr(), rows, cols, wide, rows, 1, _FP8[format]))
+
+
+def _like(t: torch.Tensor, dev: int, dtype: torch.dtype, shape):
+    """The row stride of a matrix of this type and shape on the device, or None."""
+    try:
+        ld, one = t.stride()
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and (one == 1 or shape[1] <= 1):
+            return ld if shape[0] > 1 else shape[1]
+    except (AttributeError, TypeError, ValueError):
+        pass
+    return None
+
+
 def fobq_fp8_rms_norm(ctx: int, x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
                       format: torch.dtype = torch.float8_e4m3fn, out: Optional[Fp8Matrix] = None, sum: Optional[torch.Tensor] = None,
                       norm: Optional[torch.Tensor] = None):
@@ -700,24 +729,28 @@ def fobq_fp8_rms_norm(ctx: int, x: torch.Tensor, weight: Optional[torch.Tensor] 
     x + residual, new, or into the tensor given (which may be x or residual); None without a residual if none is given.  norm: filled with the
     norm in x's type, if given.  No gradient passes it."""
     _need(x, ctx, _FLOAT, 2, "x")
-    rows, cols = x.shape
-    dtype, device = x.dtype, x.device
-    if weight is not None and (_need(weight, ctx, (dtype, torch.float32), 1, "weight").shape[0] != cols):
-        raise TypeError(f"weight: need {cols} entries, got {weight.shape[0]}")
+    shape, dtype, device, wtype = x.shape, x.dtype, x.device, x.dtype
+    rows, cols = shape
+    dev = device.index
+    if weight is not None:
+        wtype = weight.dtype
+        if (wtype is not dtype and wtype is not torch.float32) or weight.shape != (cols,) or weight.get_device() != dev or not weight.is_contiguous():
+            _need(weight, ctx, (dtype, torch.float32), 1, "weight")
+            raise TypeError(f"weight: need {cols} entries, got {weight.shape[0]}")
     if residual is not None and sum is None:
-        sum = _empty(ctx, (rows, cols), dtype, device)
-    lds = []
-    for name, t in (("residual", residual), ("sum", sum), ("norm", norm)):
-        if t is None:
-            lds.append(cols)
-            continue
-        if _need(t, ctx, (dtype,), 2, name).shape != x.shape:
-            raise TypeError(f"{name}: need {rows} x {cols}, got {tuple(t.shape)}")
-        lds.append(t.stride()[0] if rows > 1 else cols)
-    out, m = _out_fp8(ctx, out, rows, cols, format, 1, device)
+        sum = _new(ctx, rows, cols, dtype, device)
+    lds = [cols, cols, cols]
+    for i, t in enumerate((residual, sum, norm)):
+        if t is not None:
+            lds[i] = _like(t, dev, dtype, shape)
+            if lds[i] is None:
+                name = ("residual", "sum", "norm")[i]
+                _need(t, ctx, (dtype,), 2, name)
+                raise TypeError(f"{name}: need {rows} x {cols}, got {tuple(t.shape)}")
+    out, m = _new_rows(ctx, rows, cols, format, device) if out is None else _out_fp8(ctx, out, rows, cols, format, 1, device)
     n = _norm(x.data_ptr(), residual.data_ptr() if residual is not None else 0, weight.data_ptr() if weight is not None else 0,
               sum.data_ptr() if sum is not None else 0, norm.data_ptr() if norm is not None else 0, x.stride()[0] if rows > 1 else cols, *lds,
-              _FLOAT[dtype], _FLOAT[weight.dtype] if weight is not None else _FLOAT[dtype], eps, 0)
+              _FLOAT[dtype], _FLOAT[wtype], eps, 0)
     _check(ctx, load_library().fobq_fp8_rms_norm(ctx, n, m))
     return out, sum
 
@@ -728,7 +761,8 @@ def fobq_fp8_swiglu(ctx: int, x: torch.Tensor, format: torch.dtype = torch.float
     rows, both = x.shape
     if both % 2:
         raise TypeError(f"x: need an even number of columns, got {both}")
-    out, m = _out_fp8(ctx, out, rows, both // 2, format, 1, x.device)
+    cols = both // 2
+    out, m = _new_rows(ctx, rows, cols, format, x.device) if out is None else _out_fp8(ctx, out, rows, cols, format, 1, x.device)
     _check(ctx, load_library().fobq_fp8_swiglu(ctx, x.data_ptr(), _FLOAT[x.dtype], x.stride()[0] if rows > 1 else both, m))
     return out
 
@@ -775,8 +809,12 @@ def fobq_route(ctx: int, logits: torch.Tensor, top_k: int, *, score: str = "soft
         raise TypeError(f"top_k must be in 1..{min(32, experts)}, got {top_k}")
     i32, f32, device = torch.int32, torch.float32, logits.device
     if out is None:
-        out = Routing(_empty(ctx, (tokens, top_k), i32, device), _empty(ctx, (tokens, top_k), f32, device), _empty(ctx, (experts + 1,), i32, device),
-                      _empty(ctx, (tokens * top_k,), i32, device), _empty(ctx, (tokens, top_k), i32, device))
+        # the whole numbers in one allocation: a view takes half of one's time
+        size = tokens * top_k
+        whole, weights = _new(ctx, 1, 3 * size + experts + 1, i32, device), _new(ctx, tokens, top_k, f32, device)
+        two = (tokens, top_k), (top_k, 1)
+        out = Routing(whole.as_strided(*two, 0), weights, whole.as_strided((experts + 1,), (1,), 3 * size), whole.as_strided((size,), (1,), size),
+                      whole.as_strided(*two, 2 * size))
         to = _routing(out.chosen.data_ptr(), out.weights.data_ptr(), out.starts.data_ptr(), out.pairs.data_ptr(), out.places.data_ptr())
     else:
         to = _routing(_dense(out.chosen, ctx, i32, (tokens, top_k), "chosen"), _dense(out.weights, ctx, f32, (tokens, top_k), "weights"),
@@ -847,7 +885,7 @@ def fobq_fp8_expert_matmul(ctx: int, A: Fp8Matrix, experts: Fp8Experts, routing:
     if out is None:
         if dtype not in _FLOAT:
             raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-        out = _empty(ctx, (rows, n), dtype, device)
+        out = _new(ctx, rows, n, dtype, device)
     else:
         _need(out, ctx, _FLOAT, 2, "out")
         if tuple(out.shape) != (rows, n):
@@ -865,16 +903,21 @@ def fobq_expert_sum(ctx: int, y: torch.Tensor, routing: Routing, base: Optional[
     (rows, cols), dtype = y.shape, y.dtype
     if routing.places.dim() != 2:
         raise TypeError(f"places: need tokens x top_k, got {tuple(routing.places.shape)}")
-    tokens, top_k = routing.places.shape
-    places, weights = _dense(routing.places, ctx, torch.int32, (tokens, top_k), "places"), _dense(routing.weights, ctx, torch.float32, (tokens, top_k), "weights")
+    shape, device = routing.places.shape, y.device
+    tokens, top_k = shape
+    places, weights = _dense(routing.places, ctx, torch.int32, shape, "places"), _dense(routing.weights, ctx, torch.float32, shape, "weights")
     if out is None:
-        out = _empty(ctx, (tokens, cols), dtype, y.device)
-    for name, t in (("out", out), ("base", base)):
-        if t is not None and _need(t, ctx, (dtype,), 2, name).shape != (tokens, cols):
-            raise TypeError(f"{name}: need {tokens} x {cols}, got {tuple(t.shape)}")
+        out = _new(ctx, tokens, cols, dtype, device)
+    lds = [cols, cols]
+    for i, t in enumerate((out, base)):
+        if t is not None:
+            lds[i] = _like(t, device.index, dtype, (tokens, cols))
+            if lds[i] is None:
+                name = ("out", "base")[i]
+                _need(t, ctx, (dtype,), 2, name)
+                raise TypeError(f"{name}: need {tokens} x {cols}, got {tuple(t.shape)}")
     _check(ctx, load_library().fobq_expert_sum(ctx, y.data_ptr(), _FLOAT[dtype], rows, cols, y.stride()[0] if rows > 1 else cols, weights, places, tokens, top_k,
-                                               base.data_ptr() if base is not None else None, base.stride()[0] if base is not None and tokens > 1 else cols,
-                                               out.data_ptr(), out.stride()[0] if tokens > 1 else cols))
+                                               base.data_ptr() if base is not None else None, lds[1], out.data_ptr(), lds[0]))
     return out
 
 
