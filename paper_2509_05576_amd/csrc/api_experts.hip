@@ -85,7 +85,7 @@ static int check_experts(fobq_ctx* ctx, const fobq_fp8_matrix* A, const fobq_fp8
     if (!is_float(type)) return set_err(ctx, FOBQ_EINVAL, "unknown type %d", type);
     if (ld < b.rows) return set_err(ctx, FOBQ_EINVAL, "ld (%lld) is less than the rows of B", (long long)ld);
     *p = expert_plan(ctx ? ctx->cus : 256, rows, B->experts, b.rows, a.cols, type, b.per);
-    if (p->tiles * (p->tm == 16 || p->tn == 256 ? 2 : 1) > MAX_TILES)      // (those have 512 threads)
+    if (p->tiles * (p->tm == 16 || p->tn == 256 || p->parts == 2 ? 2 : 1) > MAX_TILES)      // (those have 512 threads)
         return set_err(ctx, FOBQ_EINVAL, "Y may have more than %lld tiles of %d", (long long)MAX_TILES, p->tm);
     *v = ExpertView{a, b, B->experts, B->expert_values, B->expert_scales, starts, pairs, top_k, (int)rows, nullptr, type, ld};
     return FOBQ_OK;

@@ -116,14 +116,20 @@ __device__ __forceinline__ void copy16_from(const uint8_t* src, void* lds_base)
 }
 
 // TM x TN outputs by WM x WN wavefronts, the tiles of STAGES - 1 blocks under way.  FA, FB: the types of A and B; PER: rows of B to a scale.
-template <int TM, int TN, int WM, int WN, int STAGES, int FA, int FB, int PER, bool EXACT>
-__global__ __launch_bounds__(64 * WM * WN) void fp8_experts_kernel(ExpertView g)
+// (32768 rows in 64 experts of 4096 x 2048, bf16, a scale per 128 x 128: 381 us, 1.44 PFLOP/s, in tiles of 256 x 256; with 512 rows in each expert 319, as one
+// product of as many rows in whole tiles takes 302.  A tile's 16 blocks take 33 us, its start and end 6, of which the stores 4.7; a block 2.06, its products
+// alone 1.47, its copies alone 1.71: LDS has both.  256 rows in 128 experts of 2048 x 2048: 80 us, 5.4 TB/s.)
+// With PARTS above 1 as many such sets of wavefronts deal the blocks of columns among them, and add up in LDS, in their order.
+template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, int FA, int FB, int PER, bool EXACT>
+__global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(ExpertView g)
 {
     constexpr int WAVES = WM * WN, THREADS = 64 * WAVES, SM = TM / WM / 16, SN = TN / WN / 16;
     // per stage: rows of A, rows of B, and the scales of each
     constexpr int ROWS = TM + TN, STAGE = ROWS * 132;
-    __shared__ __attribute__((aligned(16))) uint8_t sh[STAGES][STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) uint8_t all[PARTS][STAGES][STAGE];
+    const int tid = threadIdx.x % THREADS, lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint8_t(*const sh)[STAGE] = all[part];
     const int q = lane >> 4, c = lane & 15;
     const int wm = wave / WN, wn = wave % WN;
     const int N = g.b.rows, K = g.a.cols, blocks = (K + 127) / 128;
@@ -138,7 +144,7 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_experts_kernel(ExpertView g)
     // Rows of A behind the tile's last are that one again, and not stored; rows of B behind its last read as zeros.
     constexpr int PA = TM * 8 / THREADS, PB = TN * 8 / THREADS, STEP = THREADS / 8;
     static_assert(TM % STEP == 0 && TN % STEP == 0 && STEP % 16 == 0, "pieces of whole rows, the same place in each");
-    const int row = threadIdx.x >> 3, column = swizzle(row, threadIdx.x & 7) * 16;
+    const int row = tid >> 3, column = swizzle(row, tid & 7) * 16;
     int at_a[PA];
 #pragma unroll
     for (int i = 0; i < PA; ++i) at_a[i] = row_of_a(g, p0 + min(i * STEP + row, M - 1));
@@ -157,19 +163,19 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_experts_kernel(ExpertView g)
     const float* const scale_of = (of_a ? g.a.scales : b_scales) + scale0;
     const int64_t scale_ld = of_a ? g.a.ld_scales : g.b.ld_scales;
     // (the tile's own part of B needs no rows of A to be known)
-    const int whole = K / 128;                               // blocks that are whole
-    if (whole > 0) fetch_b(0, 0);
+    const int whole = K / 128, mine = (whole - part + PARTS - 1) / PARTS, steps = (whole + PARTS - 1) / PARTS;     // blocks that are whole, and the part's
+    auto block = [&](int i) { return part + PARTS * i; };
+    if (mine > 0) fetch_b(0, block(0));
     const uint8_t* a_row[PA];
 #pragma unroll
     for (int i = 0; i < PA; ++i) a_row[i] = g.a.values + (int64_t)max(at_a[i], 0) * g.a.ld;
-    auto fetch_a = [&](int stage, int kb) {
+    auto fetch_a = [&](int stage, int kb, auto pieces) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < PA; ++i) copy16_from(a_row[i] + column + kb * 128, &sh[stage][(i * THREADS + wave * 64) * 16]);
+        for (int i = 0; i < decltype(pieces)::value; ++i) copy16_from(a_row[i] + column + kb * 128, &sh[stage][(i * THREADS + wave * 64) * 16]);
     };
     auto fetch_scales = [&](int stage, int kb) {
         copy4(run_of(scale_of + kb * scale_ld, (int64_t)scales_there * 4), scale_at * 4, &sh[stage][ROWS * 128 + piece * 256]);
     };
-    constexpr int COPIES = PA + PB + 1;
     // the last block of columns where it is not whole: what is behind it counts as zero, whatever the rows hold there
     auto fetch_rest = [&](int stage, int kb) {
         const int k = kb * 128 + column, left = K - k;
@@ -186,10 +192,10 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_experts_kernel(ExpertView g)
             __builtin_memcpy(__builtin_assume_aligned(dst, 16), w, 16);
         };
 #pragma unroll
-        for (int i = 0; i < PA; ++i) put(a_row[i], true, &sh[stage][(i * THREADS + threadIdx.x) * 16]);
+        for (int i = 0; i < PA; ++i) put(a_row[i], true, &sh[stage][(i * THREADS + tid) * 16]);
         for (int i = 0; i < PB; ++i) {
             const int at = n0 + i * STEP + row;
-            put(b_values + at * g.b.ld, at < N, &sh[stage][TM * 128 + (i * THREADS + threadIdx.x) * 16]);
+            put(b_values + at * g.b.ld, at < N, &sh[stage][TM * 128 + (i * THREADS + tid) * 16]);
         }
     };
     const int place0 = swizzle(c, 2 * q) * 16, place1 = swizzle(c, 2 * q + 1) * 16;
@@ -250,40 +256,65 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_experts_kernel(ExpertView g)
             }
         }
     };
+    // By groups of a wavefront: no rows of A behind them are copied either.
     auto product = [&](auto groups) __attribute__((always_inline)) {
+        constexpr int USED = (decltype(groups)::value * 16 * WM + STEP - 1) / STEP, COPIES = USED + PB + 1;
+        constexpr auto pieces = std::integral_constant<int, USED>();
 #pragma unroll
         for (int k = 0; k < STAGES - 1; ++k)
-            if (k < whole) {
-                if (k > 0) fetch_b(k, k);
-                fetch_a(k, k);
-                fetch_scales(k, k);
+            if (k < mine) {
+                if (k > 0) fetch_b(k, block(k));
+                fetch_a(k, block(k), pieces);
+                fetch_scales(k, block(k));
             }
         int stage = 0;
-        for (int kb = 0; kb < whole; ++kb) {
-            if (kb + STAGES - 2 < whole) wait_and_meet<(STAGES - 2) * COPIES>();
+        for (int i = 0; i < steps; ++i) {
+            if (i + STAGES - 2 < mine) wait_and_meet<(STAGES - 2) * COPIES>();
             else wait_and_meet<0>();
             // everybody is done with the block before: its stage is free
-            if (kb + STAGES - 1 < whole) {
+            if (i + STAGES - 1 < mine) {
                 const int free = stage == 0 ? STAGES - 1 : stage - 1;
-                fetch_b(free, kb + STAGES - 1);
-                fetch_a(free, kb + STAGES - 1);
-                fetch_scales(free, kb + STAGES - 1);
+                fetch_b(free, block(i + STAGES - 1));
+                fetch_a(free, block(i + STAGES - 1), pieces);
+                fetch_scales(free, block(i + STAGES - 1));
             }
-            multiply(stage, groups);
+            if (PARTS == 1 || i < mine) multiply(stage, groups);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
         }
         if (whole < blocks) {
             wait_and_meet<0>();
-            fetch_rest(0, whole);
-            fetch_scales(0, whole);
+            if (part == 0) {
+                fetch_rest(0, whole);
+                fetch_scales(0, whole);
+            }
             wait_and_meet<0>();
-            multiply(0, groups);
+            if (part == 0) multiply(0, groups);
         }
     };
-    // A tile with few rows takes less: by halves (of a wavefront's groups; the whole workgroup goes the same way).
-    if (SM >= 2 && M <= TM / 2) product(std::integral_constant<int, (SM + 1) / 2>());
-    else product(std::integral_constant<int, SM>());
+    // A tile with few rows takes less: by quarters (the whole workgroup goes the same way).
+    if constexpr (SM % 4 == 0 && !EXACT) {
+        if (M <= TM / 4) product(std::integral_constant<int, SM / 4>());
+        else if (M <= TM / 2) product(std::integral_constant<int, SM / 2>());
+        else if (M <= TM / 4 * 3) product(std::integral_constant<int, SM / 4 * 3>());
+        else product(std::integral_constant<int, SM>());
+    } else {
+        if (SM >= 2 && M <= TM / 2) product(std::integral_constant<int, (SM + 1) / 2>());
+        else product(std::integral_constant<int, SM>());
+    }
 
+    if constexpr (PARTS > 1) {
+        static_assert((PARTS - 1) * SM * SN * THREADS * 16 <= sizeof all, "room for the sums");
+        f4* const sums = reinterpret_cast<f4*>(&all[0][0][0]);
+        wait_and_meet<0>();
+        if (part > 0) {
+#pragma unroll
+            for (int i = 0; i < SM * SN; ++i) sums[((part - 1) * SM * SN + i) * THREADS + tid] = acc[i / SN][i % SN];
+        }
+        wait_and_meet<0>();
+        if (part > 0) return;
+#pragma unroll
+        for (int k = 0; k < (PARTS - 1) * SM * SN; ++k) acc[k / SN % SM][k % SN] += sums[k * THREADS + tid];
+    }
     // four consecutive n of a lane's row of each group
 #pragma unroll
     for (int i = 0; i < SM; ++i) {
@@ -404,8 +435,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_experts_few_kernel(ExpertV
 //   16, 64 x 64, 64 x 128    1 token to 2 of 8 experts of 4096 x 4096: 9.3, 14.3, 18.1; 8 to 3 of 7 of 1000 x 2304: 7.2, 9.6, 11.5; 32: 10.2, 9.7, 11.7;
 //                            8 to 4 of 64 of 1024 x 2048: 15.6, 11.8, 11.8; 32 to 8 of 128 of 2048 x 2048: 132, 86, 80 (memory)
 //   64 x 64, 64 x 128        7 experts of 1000 x 2304, 143 rows: 13.7, 15.9; 439 rows: 25.9, 20.6
-//   64 x 128, 128 x 256, 256 x 256   64 experts of 4096 x 2048, 128 rows: -, 160, 177; 512 rows: -, 438, 383; 8 of 4096 x 4096, 83 rows: 31, 40, 58;
-//                            256 rows: 72, 75, 62; 1024 rows: 228, 183, 184; 64 of 1024 x 2048, 256 rows: 74, 66, 70
+//   64 x 64, its blocks dealt to two sets of wavefronts   7 experts of 1000 x 2304, 14, 55 and 143 rows: 9.4, 11.0, 13.3 with one, 8.2, 9.6, 13.0 with two (fp32 and a
+//                            scale per row: 11.6, 15.1, 22.3 and 10.4, 13.3, 20.2); 4 of 3000 x 1000, 83 rows: 9.4 and 10.2
+//   64 x 128, 128 x 256, 256 x 256   64 experts of 4096 x 2048, 128 rows: 193, 155, 171; 512 rows: 560, 432, 381; 8 of 4096 x 4096, 83 rows: 31, 40, 58;
+//                            256 rows: 72, 75, 62; 1024 rows: 233, 187, 187; 64 of 1024 x 2048, 256 rows: 74, 66, 70
 //   fp32, 64 x 128, 128 x 128, 128 x 256   8 of 4096 x 4096, 1024 rows: 365, 321, 352; 128 of 2048 x 2048, 64 rows: 168, 170, 166
 // The larger ones are chosen by rounds of workgroups (two of 64 x 128 or 128 x 128 on a compute unit at a time, one of the others), a round of 128 x 256
 // taking 1.45 times as long as one of 64 x 128, 1.57 with a scale per row of B, one of 256 x 256 2.45 times, one of 128 x 128 in fp32 1.6 times.
@@ -415,10 +448,12 @@ ExpertPlan expert_plan(int cus, int64_t rows, int experts, int64_t n, int64_t k,
     auto tiles = [&](int tm, int tn) { return std::max(with_rows, rows / tm + with_rows / 2) * ((n + tn - 1) / tn); };
     auto rounds = [&](int tm, int tn, int at_once) { return (double)((tiles(tm, tn) + at_once * cus - 1) / (at_once * cus)); };
     ExpertPlan p;
+    p.parts = 1;
     if (rows <= 8 * with_rows && tiles(64, 64) < cus) {
         p.tm = p.tn = 16;
     } else if (tiles(64, 128) < cus) {
         p.tm = p.tn = 64;
+        if (k >= 2048 && 2 * tiles(64, 64) <= 3 * cus) p.parts = 2;
     } else {
         p.tm = 64;
         p.tn = 128;
@@ -443,17 +478,22 @@ static hipError_t experts_of(hipStream_t s, const ExpertPlan& p, const ExpertVie
     if (p.tm == 16) {
         hipLaunchKernelGGL((fp8_experts_few_kernel<FA, FB, PER>), grid, dim3(64 * FEW_WAVES), 0, s, g);
     } else if (p.tm == 64 && p.tn == 64) {
-        if (exact) hipLaunchKernelGGL((fp8_experts_kernel<64, 64, 2, 2, 4, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
-        else hipLaunchKernelGGL((fp8_experts_kernel<64, 64, 2, 2, 4, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+        if (p.parts == 2) {
+            if (exact) hipLaunchKernelGGL((fp8_experts_kernel<64, 64, 2, 2, 2, 2, FA, FB, PER, true>), grid, dim3(512), 0, s, g);
+            else hipLaunchKernelGGL((fp8_experts_kernel<64, 64, 2, 2, 2, 2, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
+        } else {
+            if (exact) hipLaunchKernelGGL((fp8_experts_kernel<64, 64, 2, 2, 4, 1, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
+            else hipLaunchKernelGGL((fp8_experts_kernel<64, 64, 2, 2, 4, 1, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+        }
     } else if (p.tm == 64) {
-        if (exact) hipLaunchKernelGGL((fp8_experts_kernel<64, 128, 1, 4, 3, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
-        else hipLaunchKernelGGL((fp8_experts_kernel<64, 128, 1, 4, 3, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
+        if (exact) hipLaunchKernelGGL((fp8_experts_kernel<64, 128, 1, 4, 3, 1, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
+        else hipLaunchKernelGGL((fp8_experts_kernel<64, 128, 1, 4, 3, 1, FA, FB, PER, false>), grid, dim3(256), 0, s, g);
     } else if (exact) {
-        hipLaunchKernelGGL((fp8_experts_kernel<128, 128, 2, 2, 2, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
+        hipLaunchKernelGGL((fp8_experts_kernel<128, 128, 2, 2, 2, 1, FA, FB, PER, true>), grid, dim3(256), 0, s, g);
     } else if (p.tm == 128) {
-        hipLaunchKernelGGL((fp8_experts_kernel<128, 256, 2, 4, 3, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
+        hipLaunchKernelGGL((fp8_experts_kernel<128, 256, 2, 4, 3, 1, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
     } else {
-        if constexpr (PER == 128) hipLaunchKernelGGL((fp8_experts_kernel<256, 256, 2, 4, 2, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
+        if constexpr (PER == 128) hipLaunchKernelGGL((fp8_experts_kernel<256, 256, 2, 4, 2, 1, FA, FB, PER, false>), grid, dim3(512), 0, s, g);
     }
     return hipGetLastError();
 }

@@ -57,14 +57,15 @@ struct RouteView {
 };
 hipError_t launch_route(hipStream_t s, const RoutePlan& p, const RouteView& g, int type, int32_t* work);
 
-// The products of experts' rows: b is expert 0's matrix, the others lie behind it.  tm, tn: packed rows and rows of B to a workgroup; tiles: workgroups
+// The products of experts' rows: b is expert 0's matrix, the others lie behind it.  tm, tn: packed rows and rows of B to a workgroup; parts: sets of
+// wavefronts that deal its blocks of columns among them; tiles: workgroups
 // that all tiles fit in, however the packed rows are dealt among the experts.
 struct ExpertView {
     Fp8View a, b; int experts; int64_t expert_values, expert_scales;
     const int32_t *starts, *pairs; int top, rows;
     void* y; int type; int64_t ldy;
 };
-struct ExpertPlan { int tm, tn; int64_t tiles; };
+struct ExpertPlan { int tm, tn, parts; int64_t tiles; };
 ExpertPlan expert_plan(int cus, int64_t rows, int experts, int64_t n, int64_t k, int type, int per);
 hipError_t launch_expert_matmul(hipStream_t s, const ExpertPlan& p, const ExpertView& g);
 
