@@ -733,7 +733,7 @@ def fobq_fp8_rms_norm(ctx: int, x: torch.Tensor, weight: Optional[torch.Tensor] 
     rows, cols = shape
     dev = device.index
     if weight is not None:
-        wtype = weight.dtype
+        wtype = getattr(weight, "dtype", None)
         if (wtype is not dtype and wtype is not torch.float32) or weight.shape != (cols,) or weight.get_device() != dev or not weight.is_contiguous():
             _need(weight, ctx, (dtype, torch.float32), 1, "weight")
             raise TypeError(f"weight: need {cols} entries, got {weight.shape[0]}")
@@ -875,8 +875,8 @@ def fobq_fp8_expert_matmul(ctx: int, A: Fp8Matrix, experts: Fp8Experts, routing:
     b, count, n, k2 = _experts(ctx, experts)
     if k != k2:
         raise TypeError(f"A has {k} columns, the experts {k2}")
-    pairs, places = routing.pairs, routing.places
-    if places.dim() != 2 or pairs.dim() != 1 or places.numel() != pairs.shape[0]:
+    pairs, places = _need(routing.pairs, ctx, _I32, 1, "pairs"), _need(routing.places, ctx, _I32, 2, "places")
+    if places.numel() != pairs.shape[0]:
         raise TypeError(f"routing: need places tokens x top_k and as many pairs, got {tuple(places.shape)} and {tuple(pairs.shape)}")
     (tokens, top_k), rows = places.shape, pairs.shape[0]
     if m != (rows if packed else tokens):
@@ -901,9 +901,7 @@ def fobq_expert_sum(ctx: int, y: torch.Tensor, routing: Routing, base: Optional[
     or into `out`, which may be base.  No gradient passes it."""
     _need(y, ctx, _FLOAT, 2, "y")
     (rows, cols), dtype = y.shape, y.dtype
-    if routing.places.dim() != 2:
-        raise TypeError(f"places: need tokens x top_k, got {tuple(routing.places.shape)}")
-    shape, device = routing.places.shape, y.device
+    shape, device = _need(routing.places, ctx, _I32, 2, "places").shape, y.device
     tokens, top_k = shape
     places, weights = _dense(routing.places, ctx, torch.int32, shape, "places"), _dense(routing.weights, ctx, torch.float32, shape, "weights")
     if out is None:

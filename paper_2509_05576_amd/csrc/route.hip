@@ -245,8 +245,16 @@ __device__ __forceinline__ void route_logits(const RouteView& g, const RouteLane
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(1.44269504f * x); }
 
+// exp(x) to 3 units for x that is not positive (0 from -200 on): 2^t 2^rest, t the product with log2(e) rounded to fp32, rest what that leaves out.
+__device__ __forceinline__ float exp_fine(float x)
+{
+    x = fmaxf(x, -200.f);
+    const float t = 1.44269504f * x, rest = fmaf(1.92596299e-8f, x, fmaf(1.44269504f, x, -t)), e = __builtin_amdgcn_exp2f(t);
+    return fmaf(e, 0.693147181f * rest, e);
+}
+
 // A slot's weight from its logit z (-Inf: none), before the scale.  over(x) and sum(x): the largest and the sum over the token's lanes; most and total: the row's
-// largest logit and the sum of exp(x - most), for a softmax that is not renormalized.  exp2 and its argument's rounding are off by (|x| + 2) units.
+// largest logit and the sum of exp(x - most), for a softmax that is not renormalized.
 template <class Over, class Sum>
 __device__ __forceinline__ float route_weight(const RouteView& g, float z, float most, float total, Over over, Sum sum)
 {
@@ -254,17 +262,18 @@ __device__ __forceinline__ float route_weight(const RouteView& g, float z, float
     float p = 0.f;
     if (g.score == FOBQ_SOFTMAX) {
         const float top = g.renormalize ? over(z) : most;
-        if (there) p = exp_of(z - top);
-        return p * __builtin_amdgcn_rcpf(g.renormalize ? sum(p) : total);
+        if (there) p = exp_fine(z - top);
+        return p / (g.renormalize ? sum(p) : total);
     }
-    if (there) p = __builtin_amdgcn_rcpf(1.f + exp_of(-z));
+    const float e = exp_fine(-fabsf(z));
+    if (there) p = (z < 0.f ? e : 1.f) / (1.f + e);
     if (!g.renormalize) return p;
     const float top = over(z);
     if (__ballot(top < -60.f)) {
         // relative to the largest, where the scores themselves are too small for fp32
-        if (there && top < -60.f) p = exp_of(z - top);
+        if (there && top < -60.f) p = exp_fine(z - top);
     }
-    return p * __builtin_amdgcn_rcpf(sum(p));
+    return p / sum(p);
 }
 
 // A token's experts and weights, lane s those of slot s.  SCORED: scores are compared, not logits.
@@ -333,7 +342,7 @@ __device__ __forceinline__ Choice route_token(const RouteView& g, const RouteLan
     float total = 0.f;
     if (g.score == FOBQ_SOFTMAX && !g.renormalize) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) total += logit[j] == none ? 0.f : exp_of(logit[j] - most);
+        for (int j = 0; j < V; ++j) total += logit[j] == none ? 0.f : exp_fine(logit[j] - most);
         total = wave_sum(total);
     }
     const float p = route_weight(g, z, most, total, [](float x) { return value_of(wave_most(order_of(x))); }, [](float x) { return wave_sum(x); });

@@ -107,6 +107,22 @@ def test_every_tile(ctx, per_expert, per):
         check(ctx, _matrix(ctx, r.pairs.shape[0], k, E4, 1, 4), w, r, dtype, True)
 
 
+@pytest.mark.parametrize("form,counts,n,per,dtype", [
+    ((16, 16), [1, 3, 0, 2], 200, 128, BF), ((16, 16), [1, 0, 17, 2], 200, 1, F32), ((64, 64), [20, 5, 64, 31], 1000, 128, BF), ((64, 64), [20, 5, 64, 31], 1000, 1, F32),
+    ((64, 128), [70, 0, 300, 130], 4100, 128, HF), ((64, 128), [70, 0, 300, 130], 4100, 1, F32), ((128, 256), [500, 31, 0, 669], 4100, 128, BF),
+    ((128, 256), [129, 450, 64, 557], 4100, 1, HF), ((128, 128), [1500, 500, 7, 1993], 4100, 128, F32), ((128, 128), [1500, 500, 7, 1993], 4100, 1, F32),
+    ((256, 256), [1000, 64, 700, 636], 4100, 128, BF), ((256, 256), [129, 1281, 193, 797], 4100, 128, HF)])
+@pytest.mark.parametrize("k", [128, 300, 2100])
+def test_forms(ctx, form, counts, n, per, dtype, k):
+    """Each form of the product, as the rules choose it, with tiles that are full, that have a quarter, half or three of their rows, and one."""
+    import paper_2509_05576_amd as fobq
+    types = {F32: 0, BF: 1, HF: 2}
+    rows = sum(counts)
+    assert fobq.fobq_debug_plan(fobq.PLAN_EXPERTS, [torch.cuda.get_device_properties(0).multi_processor_count, rows, len(counts), n, k, types[dtype], per], 3)[:2] == list(form)
+    r = _routing(counts, 1)
+    check(ctx, _matrix(ctx, rows, k, E4, 1, 5), _weights(ctx, len(counts), n, k, E4, per), r, dtype, False)
+
+
 def test_pairs_of_no_expert(ctx):
     for counts, none in (([10, 0, 4], 4), ([0, 0], 8), ([100, 70], 30)):
         r = _routing(counts, 2, none=none)

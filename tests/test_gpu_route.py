@@ -35,7 +35,8 @@ def check(ctx, logits, top_k, **kw):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
-@pytest.mark.parametrize("experts,top_k", [(1, 1), (2, 1), (7, 3), (8, 8), (64, 6), (65, 2), (128, 8), (200, 32), (256, 8), (500, 5), (513, 4), (1024, 10)])
+@pytest.mark.parametrize("experts,top_k", [(1, 1), (2, 1), (7, 3), (8, 8), (64, 6), (65, 2), (128, 8), (200, 32), (256, 8), (500, 5), (513, 4), (1024, 10), (15, 15),
+                                           (16, 14), (16, 16), (32, 14), (32, 15), (256, 14), (256, 15), (257, 8)])
 def test_experts(ctx, experts, top_k, score):
     for i, (dtype, bias, renormalize) in enumerate(((F32, False, True), (BF, True, True), (HF, False, False), (F32, True, False))):
         b = 0.1 * _logits(1, experts, F32, 9)[0] if bias else None
@@ -43,7 +44,8 @@ def test_experts(ctx, experts, top_k, score):
 
 
 @pytest.mark.parametrize("experts,groups,top_groups,top_k", [(8, 2, 1, 3), (64, 8, 3, 6), (104, 8, 4, 8), (256, 8, 4, 8), (160, 5, 2, 6), (62, 31, 7, 9), (64, 64, 20, 8),
-                                                             (1024, 64, 32, 16), (990, 33, 4, 20), (48, 3, 3, 5), (12, 12, 4, 4)])
+                                                             (1024, 64, 32, 16), (990, 33, 4, 20), (48, 3, 3, 5), (12, 12, 4, 4), (256, 16, 7, 14), (256, 16, 16, 8), (272, 17, 5, 8), (250, 2, 1, 9),
+                                                             (16, 16, 3, 3), (33, 3, 2, 15)])
 def test_groups(ctx, experts, groups, top_groups, top_k):
     for i, (score, bias, group_top) in enumerate((("softmax", False, 1), ("sigmoid", True, 2), ("softmax", True, 1), ("softmax", False, 2), ("sigmoid", False, 2))):
         b = 0.1 * _logits(1, experts, F32, 3)[0] if bias else None
@@ -93,6 +95,33 @@ def test_close_keys(ctx):
     assert torch.equal(r.chosen.cpu()[sure], want[sure])
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts,groups,top_groups,top_k", [(64, 8, 3, 6), (256, 8, 4, 8), (128, 1, 1, 8), (600, 20, 7, 9), (256, 16, 2, 14)])
+def test_close_groups_and_keys(ctx, experts, groups, top_groups, top_k, score):
+    """Biases that make keys, and so the groups' sums, nearly alike for some of the tokens: where they are further apart than 64 bits round, 64 bits decide."""
+    g = torch.Generator().manual_seed(experts)
+    base = _logits(1, experts, F32, 4)[0]
+    p = torch.softmax(base.double(), 0) if score == "softmax" else torch.sigmoid(base.double())
+    bias = (0.5 - p).float()                                 # the same key for all experts, but for the bias's rounding
+    x = base.repeat(40, 1)
+    x[20:] += 0.001 * torch.randn((20, experts), generator=g)
+    r = ctx.route(x.cuda(), top_k, score=score, bias=bias.cuda(), groups=groups, top_groups=top_groups)
+    p = torch.softmax(x.double(), 1) if score == "softmax" else torch.sigmoid(x.double())
+    key, each, sure = p + bias.double(), experts // groups, 0
+    for t in range(40):
+        level = key[t].view(groups, each).sort(1, descending=True).values[:, :2].sum(1)
+        order = torch.sort(level, descending=True, stable=True)
+        apart = [float(order.values[top_groups - 1] - order.values[top_groups])] if top_groups < groups else []
+        allowed = torch.zeros(groups, dtype=torch.bool)
+        allowed[order.indices[:top_groups]] = True
+        k = key[t].masked_fill(~allowed.repeat_interleave(each), -math.inf)
+        best = torch.sort(k, descending=True, stable=True)
+        if min(apart + (best.values[:top_k] - best.values[1:top_k + 1]).tolist()) > 1e-14:
+            assert torch.equal(r.chosen[t].cpu(), best.indices[:top_k].to(torch.int32)), t
+            sure += 1
+    assert sure > 15
+
+
 def test_far_logits(ctx):
     """Scores that no type holds: chosen by their logits, weights relative to the largest."""
     x = _logits(20, 30, F32, 5, 1.0) - 3000.0
@@ -121,6 +150,12 @@ def test_masked_and_not_finite(ctx, score):
     for bad in (math.nan, math.inf):
         bias[33] = bad
         assert bool(check(ctx, x, 5, score=score, bias=bias).weights.isnan().all())
+
+
+def test_one_expert_has_all_the_weight(ctx):
+    x = _logits(50, 40, F32, 2)
+    for kw in (dict(), dict(score="sigmoid"), dict(score="sigmoid", bias=torch.linspace(0, 1, 40).cuda()), dict(score="sigmoid", groups=40, top_groups=1)):
+        assert bool((ctx.route(x.cuda(), 1, **kw).weights == 1).all())
 
 
 def test_strides_and_given_outputs(ctx):
