@@ -132,13 +132,14 @@ __global__ __launch_bounds__(512) void rms_norm_kernel(NormView g, int waves)
     }
 }
 
-// silu(gate) * up = gate up / (1 + exp(-gate)); exp(-gate) is kept below 2^126.  exp(-gate) = 2^t 2^rest: t is the product with log2(e) rounded to fp32, rest
-// what that leaves out (with t alone the result is off by |gate| units, and more values fall to the other side of an 8-bit border).  The reciprocal
-// is corrected once.
+// silu(gate) * up = gate up / (1 + exp(-gate)); exp(-gate) is kept between 2^-145 and 2^126.  exp(-gate) = 2^t 2^rest: t is the product with log2(e) rounded to
+// fp32, rest what that leaves out (with t alone the result is off by |gate| units, and more values fall to the other side of an 8-bit border).  The
+// reciprocal is corrected once.
 __device__ __forceinline__ float swiglu(float gate, float up)
 {
-    const float t = -1.44269504f * gate, rest = fmaf(-1.92596299e-8f, gate, fmaf(-1.44269504f, gate, -t));
-    float e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+    const float x = __builtin_amdgcn_fmed3f(gate, -87.33f, 100.f);           // (what is not finite comes back with the last products)
+    const float t = -1.44269504f * x, rest = fmaf(-1.92596299e-8f, x, fmaf(-1.44269504f, x, -t));
+    float e = __builtin_amdgcn_exp2f(t);
     e = fmaf(e, 0.693147181f * rest, e);
     const float d = 1.f + e;
     float r = __builtin_amdgcn_rcpf(d);

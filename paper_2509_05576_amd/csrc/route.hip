@@ -453,7 +453,7 @@ __device__ __forceinline__ Choice route_four(const RouteView& g, const RouteLane
     const int lane = threadIdx.x & 15;
     const float none = -__builtin_inff();
     float key[V], most = none, total = 0.f;
-    bool odd = l.bad;
+    bool odd = l.bad, below = false;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         key[j] = (float)raw[j];
@@ -483,19 +483,23 @@ __device__ __forceinline__ Choice route_four(const RouteView& g, const RouteLane
         range = fmaf(2.f, l.most_bias, 1.01f * inv);
         near = 0x1p-24f * ((g.score == FOBQ_SOFTMAX ? 70.f : 20.f) * inv + 4.f * l.most_bias);
     } else {
-        low = most - 16.f;
+        // (relative to the largest, so that the grid's offset is exact however far from 0 they are)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            below |= key[j] != none && !(key[j] - most >= -16.f);
+            key[j] -= most;
+        }
+        low = -16.f;
         range = 16.f;
         near = 0.f;
     }
     // (the grid's offset is rounded, but the same for all; -Inf and what is below becomes step 0, which is no expert)
-    const float unit = 8388600.f * __builtin_amdgcn_rcpf(range), offset = fmaf(-low, unit, 2.f);
+    const float unit = SCORED ? 8388600.f * __builtin_amdgcn_rcpf(range) : 8388600.f / 16.f, offset = fmaf(-low, unit, 2.f);
     const uint32_t behind = (15u - lane) << 4;
     uint32_t at[V];
-    bool below = false;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const float u = fmaf(key[j], unit, offset);
-        if constexpr (!SCORED) below |= u < 1.f && key[j] != none;
         at[j] = ((uint32_t)fmaxf(u, 0.f) << 8 | behind) | (15u - j);
     }
     if (g.groups > 1) {

@@ -150,6 +150,7 @@ def test_swiglu_extremes(ctx):
     g[:, 256:384] = torch.linspace(-95, -60, 128)
     g[0, 384], u[1, 512], g[2, 640] = math.nan, math.inf, -math.inf
     g[:, 768:896], u[:, 768:896] = 1e25, 1e25             # passes fp32
+    g[:, 896:], u[:, 896:] = torch.logspace(1, 38, 64).repeat(2) * torch.where(torch.arange(128) < 64, -1.0, 1.0), 0.5      # gates of every size
     wide = torch.cat((torch.zeros(3, 5), g, u, torch.zeros(3, 3)), 1).cuda()
     m = ctx.fp8_swiglu(wide[:, 5:5 + 2 * cols])
     y, rel, tiny = ref.swiglu(torch.cat((g, u), 1))

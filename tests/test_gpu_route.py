@@ -142,6 +142,8 @@ def test_masked_and_not_finite(ctx, score):
     x[4, 60] = math.nan
     x[5, 11] = math.inf
     x[6, :69] = -math.inf
+    x[7, ::3], x[8, :] = torch.finfo(F32).min, torch.finfo(F32).min      # masked by the lowest value: chosen where there is nothing else
+    x[9, 4:], x[10, ::2] = torch.finfo(F32).min, torch.finfo(BF).min
     for kw in (dict(), dict(renormalize=False), dict(groups=7, top_groups=2, group_top=2), dict(groups=7, top_groups=3, group_top=1)):
         check(ctx, x, 5, score=score, **kw)
         bias = 0.1 * _logits(1, 70, F32, 8)[0]
