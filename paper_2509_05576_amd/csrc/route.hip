@@ -1,8 +1,9 @@
 // Routing of tokens to experts, and the weighted sum of the experts' rows behind it.
 //
-// A wavefront has a token: its scores, the choice of groups and of experts, and the weights never leave registers.  A lane has neighbouring
-// experts, so that the lowest lane among equal ones has the lowest expert; with groups, 64 / groups lanes (rounded down to a power of two) have a group.  The
-// largest key is found top_k times, by the bits of the keys, which order as the keys do.
+// Up to 256 experts in groups that lanes can share: four tokens a wavefront, sixteen lanes a token, a key and its expert in one word
+// of 31 bits (route_tokens_by_four).  Otherwise a wavefront has a token, a lane neighbouring experts, so that the lowest lane among equal ones has the lowest expert; with groups,
+// 64 / groups lanes (rounded down to a power of two) have a group.  Scores, the choice and the weights never leave registers; the largest key is found top_k times, by bits that
+// order as the keys do.
 //
 // Where the rows lie is a counting sort that keeps the pairs' order.  A token has an expert once at most, so that the experts' rows among 64
 // tokens are bits of a word, set in any order, and a pair's rank is the number of bits below its token's: no result depends on the order
@@ -701,7 +702,10 @@ __device__ __forceinline__ void route_places(RouteShared& sh, const RouteView& g
     for (int64_t i = sh.base[1024] + (int64_t)part * (64 * ROUTE_WAVES) + tid; i < pairs; i += (int64_t)parts * (64 * ROUTE_WAVES)) g.pairs[i] = -1;
 }
 
-// All of it where one workgroup has the tokens; otherwise the choice, and how often each expert is in it.
+// All of it where one workgroup has the tokens; otherwise the choice, and how often each expert is in it.  Bound by the vector instructions of the choice, not by memory:
+// 16384 tokens x 256 fp32 logits take 15 to 18 us (17 MB, 4 us of a copy); alone, 64 tokens x 128 take 7.7 us, 64 x 256 with a bias and groups 12.6.  One workgroup for
+// more than 64 tokens saves a launch (65 x 128: 9.9 -> 8.8) but has fewer wavefronts (128 x 128: 9.9 -> 11.7,
+// 192 x 128: 10.2 -> 15.5): two launches from there on.
 template <class T, int V, bool SCORED, bool FOUR>
 __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_choose_kernel(RouteView g, RoutePlan p, int32_t* __restrict__ work)
 {
@@ -715,6 +719,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_choose_kernel(RouteVie
     else if (tid < (g.experts + 3) / 4 * 4) work[(int64_t)blockIdx.x * ((g.experts + 3) / 4 * 4) + tid] = sh.count[tid];      // (rows of whole fours)
 }
 
+// Where the pairs lie: each workgroup sums the counts of all (256 x 256 whole numbers, from the L2) and ranks its own tokens' pairs.  16384 tokens x 8 of 256: 7 us.
 __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_places_kernel(RouteView g, RoutePlan p, const int32_t* __restrict__ work)
 {
     __shared__ RouteShared sh;
@@ -744,7 +749,7 @@ __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_places_kernel(RouteVie
     route_places<false>(sh, g, t0, t1, part, p.parts);
 }
 
-// LANES lanes have 8 LANES columns of a token, its rows four at a time under way.  (32768 rows of 4096 bf16 to 8192 tokens with a base: 92 us, 4.4 TB/s.)
+// LANES lanes have 8 LANES columns of a token, its rows four at a time under way.  (32768 rows of 4096 bf16 to 8192 tokens with a base: 90 us, 4.5 TB/s.)
 template <class T, int LANES>
 __global__ __launch_bounds__(256) void expert_sum_kernel(ExpertSum g, unsigned across)
 {
