@@ -3,21 +3,23 @@
 //
 // Memory bound: a lane has 16 columns of a row, eight lanes a block, and everything between the loads and the 8-bit values stays in
 // registers.  The sum of squares is in fp64, which no row of finite values passes, so that rows of very large and very small values lose nothing.
-// The values are off by some units of fp32 when their block's largest is known; what is rounded to 8 bits is their product with largest value / largest,
-// one multiplication (fobq_fp8_quantize's quotient, rounded once, takes ten instructions and is for values that are given).
+// What is rounded to 8 bits is a value's product with largest 8-bit value / largest of the block, one multiplication (fobq_fp8_quantize's quotient, rounded once, takes ten
+// instructions and is for values that are given).  These values have been rounded to fp32 already, so that one in some 20000 (bf16 sums and weights, whose products often lie on
+// a border) to a million (fp32) falls on the other side of an 8-bit border than in 64 bits.  A factor that all of a row's values share would round
+// each of them once more and cancels out of a block: the norm keeps it out of them (in 3.3e8 values 10541 others than in 64 bits, with it 13733).
 #include "fp8.h"
 
 #include <type_traits>
 
 namespace fobq {
 
-// 16 values of a block, most the largest magnitude's bits, into 8 bits; the block's scale
+// 16 values of a block as multiples of `unit`, most the largest multiple's magnitude's bits, into 8 bits; the block's scale
 template <int FORMAT>
-__device__ __forceinline__ float put16_by(uint8_t* __restrict__ dst, int left, uint32_t most, const float* y)
+__device__ __forceinline__ float put16_by(uint8_t* __restrict__ dst, int left, uint32_t most, const float* y, float unit = 1.f)
 {
-    const float top = __uint_as_float(most), scale = top / Fp8<FORMAT>::TOP;
-    const bool fine = most < 0x7f800000u;
-    const float by = !fine ? __builtin_nanf("") : scale < FP8_TINY ? 0x1p126f : Fp8<FORMAT>::TOP / top;
+    const float top = __uint_as_float(most), largest = top * unit, scale = largest / Fp8<FORMAT>::TOP;
+    const bool fine = largest < __builtin_inff();
+    const float by = !fine ? __builtin_nanf("") : scale < FP8_TINY ? 0x1p126f * unit : Fp8<FORMAT>::TOP / top;
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = to_fp8x4<FORMAT>(y[4 * i] * by, y[4 * i + 1] * by, y[4 * i + 2] * by, y[4 * i + 3] * by);
@@ -65,7 +67,7 @@ __device__ __forceinline__ double over_lanes(double x)
 }
 
 // A row has LANES lanes, or with LANES 64 `waves` wavefronts of a workgroup, each with 16 columns a lane and piece.  (bf16 with a residual: 8192 x 8192
-// 103 us, 4.6 TB/s; 16384 x 2048 45 us, 5.3 TB/s, partly in the last-level cache; 32768 x 96 7 us.)
+// 102 us, 4.6 TB/s; 16384 x 2048 43 us, 5.4 TB/s, partly in the last-level cache; 32768 x 96 7 us.)
 template <class T, class W, int FORMAT, int LANES, int PIECES>
 __global__ __launch_bounds__(512) void rms_norm_kernel(NormView g, int waves)
 {
@@ -107,28 +109,26 @@ __global__ __launch_bounds__(512) void rms_norm_kernel(NormView g, int waves)
         squares = part[0];
         for (int w = 1; w < waves; ++w) squares += part[w];
     }
+    // 1 / rms = by 2^power, by in [1, 2]: the row takes the power, which rounds nothing, and `by`, common to all values of a block, goes into its scale.
     const double mean = squares / cols + (double)g.eps, inv = mean > 0.0 ? 1.0 / sqrt(mean) : 0.0;
-    float by = mean - mean == 0.0 ? (float)inv : __builtin_nanf("");      // an Inf or NaN in the row: NaN throughout
-    if (!(inv < 0x1p125 && inv > 0x1p-125)) {
-        // 1 / rms is not a normal fp32 number: in two factors, the first a power of two
-        const float pre = inv >= 1.0 ? 0x1p100f : 0x1p-100f;
-        by = mean - mean == 0.0 ? (float)(inv / (double)pre) : by;
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[p][i] *= pre;
-    }
+    const bool fine = mean - mean == 0.0;                                 // else an Inf or NaN in the row: NaN throughout
+    const int power = fine ? __builtin_amdgcn_frexp_exp(inv) - 1 : 0;
+    const float by = fine ? (float)ldexp(inv, -power) : __builtin_nanf("");
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
         const int col = col0 + p * step, left = cols - col;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[p][i] *= by;
+            s[p][i] = __builtin_amdgcn_ldexpf(s[p][i], power);
             if (g.weight) s[p][i] *= (float)tw[p][i];
         }
-        const float scale = put16_by<FORMAT>(g.out.values + row * g.out.ld + col, left, most_of_8(most16(s[p])), s[p]);
+        const float scale = put16_by<FORMAT>(g.out.values + row * g.out.ld + col, left, most_of_8(most16(s[p])), s[p], by);
         if ((lane & 7) == 0 && left > 0) g.out.scales[(int64_t)(col / 128) * g.out.ld_scales + row] = scale;
-        if (g.norm) put_row16(static_cast<T*>(g.norm) + row * g.norm_ld + col, left, s[p]);
+        if (g.norm) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[p][i] *= by;
+            put_row16(static_cast<T*>(g.norm) + row * g.norm_ld + col, left, s[p]);
+        }
     }
 }
 
@@ -176,7 +176,7 @@ static hipError_t norm_of(hipStream_t s, const NormView& g)
     else if (cols <= 512) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 32, 1>), rows_of(32), dim3(256), 0, s, g, 1);
     else if (cols <= 1024) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 64, 1>), rows_of(64), dim3(256), 0, s, g, 1);
     else {
-        // up to 8 wavefronts, which is what shares a row best (8192 x 8192: 8 with a piece each 103 us, 4 with two 107, 2 with four 133)
+        // up to 8 wavefronts, which is what shares a row best (8192 x 8192: 8 with a piece each 102 us, 4 with two 107, 2 with four 133)
         const int pieces = cols <= 8192 ? 1 : cols <= 16384 ? 2 : 4, waves = (cols + 1024 * pieces - 1) / (1024 * pieces);
         const dim3 grid((unsigned)g.out.rows), block(64 * waves);
         if (pieces == 1) hipLaunchKernelGGL((rms_norm_kernel<T, W, FORMAT, 64, 1>), grid, block, 0, s, g, waves);
