@@ -395,7 +395,7 @@ int fobq_fp8_rms_norm(fobq_ctx* ctx, const fobq_norm* norm, const fobq_fp8_matri
 
 /* silu(gate) * up into 8-bit blocks, silu(g) = g / (1 + exp(-g)): X (device, `type`, row stride ld elements) has out->rows rows of 2 out->cols
  * columns, the gates and behind them the ups.  In fp32, then by blocks as above (rows_per_scale 1).  A block with a gate or an up that is not finite, or with a
- * product that passes fp32, is NaN; 1 / (1 + exp(-g)) counts as no less than 2^-126. */
+ * product that passes fp32, is NaN; 1 / (1 + exp(-g)) below 2^-126 counts as 0. */
 int fobq_fp8_swiglu(fobq_ctx* ctx, const void* X, int32_t type, int64_t ld, const fobq_fp8_matrix* out);
 
 /* Which experts each token goes to.  Per token, from its logits x (one for each expert):

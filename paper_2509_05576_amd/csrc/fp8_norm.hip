@@ -132,12 +132,13 @@ __global__ __launch_bounds__(512) void rms_norm_kernel(NormView g, int waves)
     }
 }
 
-// silu(gate) * up = gate up / (1 + exp(-gate)); exp(-gate) is kept between 2^-145 and 2^126.  exp(-gate) = 2^t 2^rest: t is the product with log2(e) rounded to
+// silu(gate) * up = gate up / (1 + exp(-gate)); exp(-gate) is kept between 2^-145 and 2^127.97, whose reciprocal below 2^-126 the instruction makes 0, so that gates of
+// any size to that side give 0.  exp(-gate) = 2^t 2^rest: t is the product with log2(e) rounded to
 // fp32, rest what that leaves out (with t alone the result is off by |gate| units, and more values fall to the other side of an 8-bit border).  The
 // reciprocal is corrected once.
 __device__ __forceinline__ float swiglu(float gate, float up)
 {
-    const float x = __builtin_amdgcn_fmed3f(gate, -87.33f, 100.f);           // (what is not finite comes back with the last products)
+    const float x = __builtin_amdgcn_fmed3f(gate, -88.7f, 100.f);           // (what is not finite comes back with the last products)
     const float t = -1.44269504f * x, rest = fmaf(-1.92596299e-8f, x, fmaf(-1.44269504f, x, -t));
     float e = __builtin_amdgcn_exp2f(t);
     e = fmaf(e, 0.693147181f * rest, e);

@@ -157,3 +157,16 @@ def test_swiglu_extremes(ctx):
     y[:, 768:896] = math.inf
     y[~torch.isfinite(g)] = math.nan
     ref.check_blocks(m.values, m.scales, y, (y.abs() * rel + tiny).nan_to_num(0.0, 0.0, 0.0), E4)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF, HF])
+def test_swiglu_gates_far_below(ctx, dtype):
+    """exp(-gate) past fp32: 0 whatever the gate's size, up to the type's lowest value (65504 in fp16)."""
+    low = torch.tensor([-90.0, -100.0, -1000.0, -65504.0] + ([] if dtype == HF else [-1e10, -1e30, -1e37, torch.finfo(dtype).min]))
+    g = low.repeat(128 // len(low))[None].repeat(2, 1).to(dtype)
+    u = torch.linspace(-3.0, 3.0, 128)[None].repeat(2, 1).to(dtype)
+    g[1, 5], u[1, 5] = 4.0, 2.0                           # one that is there, beside them
+    m = ctx.fp8_swiglu(torch.cat((g, u), 1).cuda())
+    v = m.values.cpu().float()
+    assert (v[0] == 0).all() and m.scales[0, 0].item() == 2.0 ** -126
+    assert v[1, 5] == 448 and (v[1, :5] == 0).all() and (v[1, 6:] == 0).all()
