@@ -254,3 +254,30 @@ def test_memory_is_the_context_streams(monkeypatch, context_on_side):
             assert seen == [home.cuda_stream] * count
     torch.cuda.synchronize()
     c.close()
+
+
+def test_rows_far_apart(ctx):
+    """Rows 2^31 elements apart, so that the last begin past 32 bits: the same bits as of dense matrices."""
+    import paper_2509_05576_amd as fobq
+    rows, cols, apart = 3, 272, (1 << 31) + 16
+    memory, used = torch.empty(2 * apart + 4096, dtype=BF, device="cuda"), [0]
+
+    def far(t):
+        to = memory.as_strided((rows, t.shape[1]), (apart, 1), used[0])
+        used[0] += -(-t.shape[1] // 16) * 16
+        return to.copy_(t)
+
+    g = torch.Generator().manual_seed(5)
+    x, r, z = (torch.randn(rows, cols, generator=g).to(BF).cuda() for _ in range(3))
+    want, total = ctx.fp8_rms_norm(x, None, r, norm=torch.empty_like(x))
+    values = torch.empty(2 * apart + 4096, dtype=torch.uint8, device="cuda")
+    there = fobq.Fp8Matrix(values.as_strided((rows, cols), (apart, 1)).view(torch.float8_e4m3fn), torch.empty_like(want.scales), 1)
+    m, s = ctx.fp8_rms_norm(far(x), None, far(r), sum=far(z), out=there)
+    assert torch.equal(s, total) and torch.equal(m.values.view(torch.uint8), want.values.view(torch.uint8)) and torch.equal(m.scales, want.scales)
+    want, m = ctx.fp8_swiglu(x), ctx.fp8_swiglu(far(x), out=fobq.Fp8Matrix(there.values[:, :cols // 2], there.scales[:2].contiguous(), 1))
+    assert torch.equal(m.values.view(torch.uint8), want.values.view(torch.uint8)) and torch.equal(m.scales, want.scales)
+    want, routing = ctx.route(x[:, :200], 1), ctx.route(far(x)[:, :200], 1)
+    for a, b in zip((want.chosen, want.weights, want.starts, want.pairs, want.places), (routing.chosen, routing.weights, routing.starts, routing.pairs, routing.places)):
+        assert torch.equal(a, b)
+    base = far(z)
+    assert torch.equal(ctx.expert_sum(far(x), routing, base=base, out=base), ctx.expert_sum(x, want, base=z))
