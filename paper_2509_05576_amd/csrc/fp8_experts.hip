@@ -142,6 +142,11 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
 
     // A tile is copied 16 bytes a thread and piece, its rows in LDS one after another: a piece is THREADS / 8 rows below the one before.
     // Rows of A behind the tile's last are that one again, and not stored; rows of B behind its last read as zeros.
+    // The copies of the block that is fetched stand between the products of the one that is multiplied, a few to each of the first 1 / SPREAD of its groups: all in front of
+    // them, the first operands wait until the addresses of all are through.  With two stages they have to be under way by the middle, or the next block waits
+    // for them.  (32768 rows in 64 experts of 4096 x 2048: 386 -> 376 us, with a scale per row, 128 x 256, 480 -> 459; 1400 rows in 8 of 1024 x 4096 21.9 -> 20.0.  On fp16
+    // values, whose order is the compiler's, 427 -> 560: not there.)
+    constexpr int SPREAD = PARTS > 1 || EXACT ? 0 : STAGES == 2 ? 2 : 1;
     constexpr int PA = TM * 8 / THREADS, PB = TN * 8 / THREADS, STEP = THREADS / 8;
     static_assert(TM % STEP == 0 && TN % STEP == 0 && STEP % 16 == 0, "pieces of whole rows, the same place in each");
     const int row = tid >> 3, column = swizzle(row, tid & 7) * 16;
@@ -150,9 +155,12 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
     for (int i = 0; i < PA; ++i) at_a[i] = row_of_a(g, p0 + min(i * STEP + row, M - 1));
     const Run rb = run_of(b_values + n0 * g.b.ld, (N - n0) * g.b.ld);
     const unsigned ldb = (unsigned)g.b.ld, ob = row * ldb + column;
+    auto copy_b = [&](int stage, int kb, int i) __attribute__((always_inline)) {
+        copy16(rb, ob + (i * STEP) * ldb + (unsigned)kb * 128, &sh[stage][TM * 128 + (i * THREADS + wave * 64) * 16]);
+    };
     auto fetch_b = [&](int stage, int kb) {
 #pragma unroll
-        for (int i = 0; i < PB; ++i) copy16(rb, ob + (i * STEP) * ldb + (unsigned)kb * 128, &sh[stage][TM * 128 + (i * THREADS + wave * 64) * 16]);
+        for (int i = 0; i < PB; ++i) copy_b(stage, kb, i);
     };
     // A block's scales, one for each row of A and of B: 64 a wavefront.  (With fewer of them than wavefronts some are copied twice.)
     static_assert(ROWS / 64 <= WAVES, "every wavefront copies scales once");
@@ -169,9 +177,12 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
     const uint8_t* a_row[PA];
 #pragma unroll
     for (int i = 0; i < PA; ++i) a_row[i] = g.a.values + (int64_t)max(at_a[i], 0) * g.a.ld;
+    auto copy_a = [&](int stage, int kb, int i) __attribute__((always_inline)) {
+        copy16_from(a_row[i] + column + kb * 128, &sh[stage][(i * THREADS + wave * 64) * 16]);
+    };
     auto fetch_a = [&](int stage, int kb, auto pieces) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < decltype(pieces)::value; ++i) copy16_from(a_row[i] + column + kb * 128, &sh[stage][(i * THREADS + wave * 64) * 16]);
+        for (int i = 0; i < decltype(pieces)::value; ++i) copy_a(stage, kb, i);
     };
     auto fetch_scales = [&](int stage, int kb) {
         copy4(run_of(scale_of + kb * scale_ld, (int64_t)scales_there * 4), scale_at * 4, &sh[stage][ROWS * 128 + piece * 256]);
@@ -218,8 +229,8 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
 #pragma unroll
     for (int i = 0; i < SM; ++i) stored |= (unsigned)(group(i) + c < M && row_of_a(g, p0 + min(group(i) + c, M - 1)) >= 0) << i;
     // One group behind the other: while the matrix instructions of a group run, the sums of the one before are added up and the next one's operand
-    // comes from LDS.  The order is kept; the compiler's own has every instruction wait for the one before.
-    auto multiply = [&](int stage, auto groups) __attribute__((always_inline)) {
+    // comes from LDS; between(i) follows the first of them.  The order is kept; the compiler's own has every instruction wait for the one before.
+    auto multiply = [&](int stage, auto groups, auto between) __attribute__((always_inline)) {
         constexpr int G = decltype(groups)::value;
         using BF = decltype(operand<EXACT, FB>(i8v()));
         using AF = decltype(operand<EXACT, FA>(i8v()));
@@ -253,6 +264,7 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
                     for (int e = 0; e < 4; ++e) d[e] = fmaf(PER == 1 ? x[e] * sb[PER == 1 ? j : 0][e] : x[e], s, d[e]);
                 }
                 if (!EXACT) __builtin_amdgcn_sched_barrier(0);
+                if (j == 0) between(i);
             }
         }
     };
@@ -267,18 +279,36 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
                 fetch_a(k, block(k), pieces);
                 fetch_scales(k, block(k));
             }
-        int stage = 0;
-        for (int i = 0; i < steps; ++i) {
+        auto nothing = [](int) __attribute__((always_inline)) {};
+        int stage = 0, i = 0;
+        if constexpr (SPREAD > 0) {
+            constexpr int OVER = (decltype(groups)::value + SPREAD - 1) / SPREAD;
+            for (; i + STAGES - 1 < steps; ++i) {
+                wait_and_meet<(STAGES - 2) * COPIES>();
+                // everybody is done with the block before: its stage is free
+                const int free = stage == 0 ? STAGES - 1 : stage - 1, next = i + STAGES - 1;
+                multiply(stage, groups, [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int k = 0; k < COPIES; ++k)
+                        if (k * OVER / COPIES == at) {
+                            if (k < PB) copy_b(free, next, k);
+                            else if (k < PB + USED) copy_a(free, next, k - PB);
+                            else fetch_scales(free, next);
+                        }
+                });
+                stage = stage == STAGES - 1 ? 0 : stage + 1;
+            }
+        }
+        for (; i < steps; ++i) {
             if (i + STAGES - 2 < mine) wait_and_meet<(STAGES - 2) * COPIES>();
             else wait_and_meet<0>();
-            // everybody is done with the block before: its stage is free
-            if (i + STAGES - 1 < mine) {
+            if (SPREAD == 0 && i + STAGES - 1 < mine) {
                 const int free = stage == 0 ? STAGES - 1 : stage - 1;
                 fetch_b(free, block(i + STAGES - 1));
                 fetch_a(free, block(i + STAGES - 1), pieces);
                 fetch_scales(free, block(i + STAGES - 1));
             }
-            if (PARTS == 1 || i < mine) multiply(stage, groups);
+            if (PARTS == 1 || i < mine) multiply(stage, groups, nothing);
             stage = stage == STAGES - 1 ? 0 : stage + 1;
         }
         if (whole < blocks) {
@@ -288,7 +318,7 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
                 fetch_scales(0, whole);
             }
             wait_and_meet<0>();
-            if (part == 0) multiply(0, groups);
+            if (part == 0) multiply(0, groups, nothing);
         }
     };
     // A tile with few rows takes less: by quarters (the whole workgroup goes the same way).
