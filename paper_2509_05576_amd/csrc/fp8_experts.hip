@@ -116,9 +116,9 @@ __device__ __forceinline__ void copy16_from(const uint8_t* src, void* lds_base)
 }
 
 // TM x TN outputs by WM x WN wavefronts, the tiles of STAGES - 1 blocks under way.  FA, FB: the types of A and B; PER: rows of B to a scale.
-// (32768 rows in 64 experts of 4096 x 2048, bf16, a scale per 128 x 128: 381 us, 1.44 PFLOP/s, in tiles of 256 x 256; with 512 rows in each expert 319, as one
-// product of as many rows in whole tiles takes 302.  A tile's 16 blocks take 33 us, its start and end 6, of which the stores 4.7; a block 2.06, its products
-// alone 1.47, its copies alone 1.71: LDS has both.  256 rows in 128 experts of 2048 x 2048: 80 us, 5.4 TB/s.)
+// (32768 rows in 64 experts of 4096 x 2048, bf16, a scale per 128 x 128: 376 us, 1.46 PFLOP/s, in tiles of 256 x 256; with 512 rows in each expert 345, as one
+// product of as many rows in whole tiles takes 302.  A tile's 16 blocks take 32 us, its start and end 6, of which the stores 4.7; a block's products alone take
+// 1.47, its copies alone 1.71: LDS has both.  256 rows in 128 experts of 2048 x 2048: 80 us, 5.4 TB/s.)
 // With PARTS above 1 as many such sets of wavefronts deal the blocks of columns among them, and add up in LDS, in their order.
 template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, int FA, int FB, int PER, bool EXACT>
 __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(ExpertView g)
