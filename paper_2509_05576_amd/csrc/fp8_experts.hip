@@ -462,13 +462,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_experts_few_kernel(ExpertV
 
 // How many packed rows an expert has is known on the device only; the rules take their average over the experts that can have any, and half a tile more
 // for the last one of each.  The measurements behind them (bf16, a scale per 128 x 128 unless it says otherwise, us; rows: the average of an expert):
-//   16, 64 x 64, 64 x 128    1 token to 2 of 8 experts of 4096 x 4096: 9.3, 14.3, 18.1; 8 to 3 of 7 of 1000 x 2304: 7.2, 9.6, 11.5; 32: 10.2, 9.7, 11.7;
-//                            8 to 4 of 64 of 1024 x 2048: 15.6, 11.8, 11.8; 32 to 8 of 128 of 2048 x 2048: 132, 86, 80 (memory)
-//   64 x 64, 64 x 128        7 experts of 1000 x 2304, 143 rows: 13.7, 15.9; 439 rows: 25.9, 20.6
-//   64 x 64, its blocks dealt to two sets of wavefronts   7 experts of 1000 x 2304, 14, 55 and 143 rows: 9.4, 11.0, 13.3 with one, 8.2, 9.6, 13.0 with two (fp32 and a
-//                            scale per row: 11.6, 15.1, 22.3 and 10.4, 13.3, 20.2); 4 of 3000 x 1000, 83 rows: 9.4 and 10.2
-//   64 x 128, 128 x 256, 256 x 256   64 experts of 4096 x 2048, 128 rows: 193, 155, 171; 512 rows: 560, 432, 381; 8 of 4096 x 4096, 83 rows: 31, 40, 58;
-//                            256 rows: 72, 75, 62; 1024 rows: 233, 187, 187; 64 of 1024 x 2048, 256 rows: 74, 66, 70
+//   16, 64 x 64, 64 x 128    1 token to 2 of 8 experts of 4096 x 4096: 9.6, 12.3, 13.1; 8 to 3 of 7 of 1000 x 2304: 7.2, 8.3, 8.8; 32: 10.2, 8.4, 10.3;
+//                            8 to 4 of 64 of 1024 x 2048: 15.6, 11.4, 11.2; 32 to 8 of 128 of 2048 x 2048: 132, 84, 80 (memory)
+//   64 x 64, 64 x 128        7 experts of 1000 x 2304, 143 rows: 12.6, 13.6; 439 rows: 23.3, 18.8
+//   64 x 64, its blocks dealt to two sets of wavefronts   7 experts of 1000 x 2304, 14, 55 and 143 rows: 8.4, 10.0, 12.6 with one, 8.3, 9.6, 13.2 with two (fp32 and a
+//                            scale per row: 11.6, 15.1, 22.3 and 10.4, 13.3, 20.2); 4 of 3000 x 1000, 83 rows: 9.1 and 10.2
+//   64 x 128, 128 x 256, 256 x 256   64 experts of 4096 x 2048, 128 rows: 181, 150, 176; 512 rows: 530, 410, 381; 8 of 4096 x 4096, 83 rows: 29, 35, 45;
+//                            256 rows: 64, 69, 58; 1024 rows: 219, 181, 178; 64 of 1024 x 2048, 256 rows: 71, 63, 66
 //   fp32, 64 x 128, 128 x 128, 128 x 256   8 of 4096 x 4096, 1024 rows: 365, 321, 352; 128 of 2048 x 2048, 64 rows: 168, 170, 166
 // The larger ones are chosen by rounds of workgroups (two of 64 x 128 or 128 x 128 on a compute unit at a time, one of the others), a round of 128 x 256
 // taking 1.45 times as long as one of 64 x 128, 1.57 with a scale per row of B, one of 256 x 256 2.45 times, one of 128 x 128 in fp32 1.6 times.
@@ -483,7 +483,7 @@ ExpertPlan expert_plan(int cus, int64_t rows, int experts, int64_t n, int64_t k,
         p.tm = p.tn = 16;
     } else if (tiles(64, 128) < cus) {
         p.tm = p.tn = 64;
-        if (k >= 2048 && 2 * tiles(64, 64) <= 3 * cus) p.parts = 2;
+        if (k >= 2048 && 2 * tiles(64, 64) <= (type == FOBQ_F32 ? 3 : 2) * cus) p.parts = 2;
     } else {
         p.tm = 64;
         p.tn = 128;
