@@ -90,7 +90,8 @@ __device__ __forceinline__ void over_group(int wide, F f, double)
 template <int V> struct RouteLane { int first, there, mine, wide, each; float bias[V], most_bias; bool bad; };
 
 // key[j]: what is chosen by, -Inf where an expert is none.  Lane s gets the index, lane * V + j, in slot s, or -1.  With slack > 0 keys and groups that are that
-// near each other may be in either order: `sure` then says that there were none, but for equal ones of the same logit and bias.
+// near each other may be in either order: `sure` then says that there were none, but for equal ones of the same logit and bias; and that nothing else is that near
+// the last one chosen, looked at or not (behind equals there may be a larger key that these do not show).
 template <int V, class K>
 __device__ __forceinline__ int choose(const K (&key)[V], const RouteView& g, const RouteLane<V>& l, float slack, const float (&logit)[V], bool& sure)
 {
@@ -101,6 +102,7 @@ __device__ __forceinline__ int choose(const K (&key)[V], const RouteView& g, con
     int who[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) at[j] = order_of(key[j]), who[j] = lane * V + j;
+    bool kept = true;
     if (g.groups > 1) {
         const K none = -(K)__builtin_inf();
         K first = none, second = none;
@@ -124,7 +126,8 @@ __device__ __forceinline__ int choose(const K (&key)[V], const RouteView& g, con
             else other = __shfl(level, o * l.wide);
             better += other > level || (other == level && o < l.mine);
         }
-        if (better >= g.top_groups)
+        kept = better < g.top_groups;
+        if (!kept)
 #pragma unroll
             for (int j = 0; j < V; ++j) at[j] = 0;
         if constexpr (sizeof(K) == 4) {
@@ -174,7 +177,20 @@ __device__ __forceinline__ int choose(const K (&key)[V], const RouteView& g, con
                         if (i % V == j) x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[j]), i / V));
                     return x;
                 };
-                if (!(of(index, logit) == of(before, logit) && of(index, l.bias) == of(before, l.bias))) sure = false;
+                const float z = of(before, logit), b = of(before, l.bias);
+                if (s < g.top) {
+                    if (!(of(index, logit) == z && of(index, l.bias) == b)) sure = false;
+                } else {
+                    const float v = value_of(last);
+                    bool other = false;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        // (sorted ones are not at their experts' places any more; those chosen earlier have been compared, which does no harm again)
+                        const bool close = SORTED ? kept && fabsf((float)key[j] - v) <= slack : at[j] != 0 && v - value_of((uint32_t)at[j]) <= slack;
+                        other |= close && !(logit[j] == z && l.bias[j] == b);
+                    }
+                    if (__ballot(other)) sure = false;
+                }
             }
         }
         if (lane == s && s < g.top) got = index;
