@@ -574,17 +574,32 @@ __device__ __forceinline__ Choice route_four(const RouteView& g, const RouteLane
         z = (float)static_cast<const T*>(g.logits)[token * g.ld + expert];
         if (SCORED && g.bias) b = g.bias[expert];
     }
-    // Neighbours that the grid does not tell apart, but for equal ones; keys below the grid where it has too few.
+    // Neighbours that the grid does not tell apart (of them those that are not equals: close); keys below the grid, or at its end, where it has too few.
     auto before = [](float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x111, 0xf, 0xf, true)); };
-    const uint32_t ahead = (uint32_t)__builtin_amdgcn_mov_dpp((int)mine, 0x111, 0xf, 0xf, true) >> 8;
+    const uint32_t ahead = (uint32_t)__builtin_amdgcn_mov_dpp((int)mine, 0x111, 0xf, 0xf, true) >> 8, step = (uint32_t)(near * unit) + 3u;
     const float z0 = before(z), b0 = before(b);
-    bool close = have && lane > 0 && ahead - (mine >> 8) <= (uint32_t)(near * unit) + 3u && !(z == z0 && b == b0);
-    const unsigned long long row = 0xffffull << (threadIdx.x & 48), fell = __ballot(below), empty = __ballot(mine <= 255u && lane <= g.top);
-    const unsigned long long unsure = __ballot(close);
+    const bool beside = have && lane > 0 && ahead - (mine >> 8) <= step;
+    bool close = beside && !(z == z0 && b == b0);
+    const int row0 = threadIdx.x & 48;
+    const unsigned long long row = 0xffffull << row0, fell = __ballot(below), empty = __ballot(mine >> 8 <= 4u && lane <= g.top);
+    const unsigned long long unsure = __ballot(close), both = 3ull << g.top << row0;
+    const bool open = (__ballot(beside) & both) == both;
+    if (__ballot(open)) {
+        // Neither the last one chosen nor the next is apart from what follows, so that there may be larger ones behind the slots, also behind equals: the choice is
+        // that of 64 bits only if all that is so near to the last one is its equal.
+        const int from = row0 + g.top - 1;
+        const float z1 = __shfl(z, from), b1 = __shfl(b, from);
+        const int s1 = __shfl((int)(mine >> 8), from);
+        bool other = false;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int s = (int)(at[j] >> 8);
+            if (s > 0 && j < l.there && abs(s - s1) <= (int)step) other |= !((float)static_cast<const T*>(g.logits)[token * g.ld + l.first + j] == z1 && l.bias[j] == b1);
+        }
+        odd |= (__ballot(other) & row) != 0 && open;
+    }
     if (unsure) {
         // The first top_k + 1 slots are put in order by 64 bits, which are all that are asked for if the last of them, or the next, is apart from the one before.
-        const unsigned mark = (unsigned)(unsure >> (threadIdx.x & 48)), both = 3u << g.top;
-        odd |= (mark & both) == both;
         if constexpr (SCORED) {
             bool other;
             const double total = g.score == FOBQ_SOFTMAX ? route_row64<T, V>(g, l.first, l.there, l.mine, l.wide, token, most, false, other) : 1.0;

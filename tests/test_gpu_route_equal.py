@@ -35,7 +35,7 @@ def _few(values, chances, tokens, experts, dtype, seed):
     return torch.tensor(values)[at].to(dtype)
 
 
-EXPERTS = [300, 600, 1000]
+EXPERTS = [40, 128, 256, 300, 600, 1000]
 
 
 @pytest.mark.parametrize("experts", EXPERTS)
