@@ -86,6 +86,10 @@ __device__ __forceinline__ void over_group(int wide, F f, double)
     for (int off = 1; off < wide; off <<= 1) f([off](double v) { return __shfl_xor(v, off); });
 }
 
+// What a group's two largest keys count as.  In fp32 it stays finite: -Inf is a group without experts, and biases near the ends of fp32 would make others that too.
+__device__ __forceinline__ float level_of(float first, float second) { return __builtin_amdgcn_fmed3f(first + second, -3.402823466e38f, 3.402823466e38f); }
+__device__ __forceinline__ double level_of(double first, double second) { return first + second; }
+
 // What is the same for all tokens of a wavefront: a lane's experts are first .. first + there - 1, group `mine` of `wide` lanes has `each`.
 template <int V> struct RouteLane { int first, there, mine, wide, each; float bias[V], most_bias; bool bad; };
 
@@ -118,7 +122,7 @@ __device__ __forceinline__ int choose(const K (&key)[V], const RouteView& g, con
         };
         if constexpr (sizeof(K) == 4) over_group(l.wide, join);
         else over_group(l.wide, join, 0.0);
-        const U level = order_of(g.group_top == 2 && second != none ? first + second : first);
+        const U level = order_of(g.group_top == 2 && second != none ? level_of(first, second) : first);
         int better = 0;
         for (int o = 0; o < g.groups; ++o) {
             U other;
@@ -453,7 +457,7 @@ __device__ __forceinline__ double route_row64(const RouteView& g, int first, int
         two = fmax(fmax(two, b), fmin(one, a));
         one = fmax(one, a);
     }
-    const double level = g.group_top == 2 && two != none ? one + two : one;
+    const double level = g.group_top == 2 && two != none ? level_of(one, two) : one;
     int better = 0;
     for (int o = 0; o < g.groups; ++o) {
         const double other = __shfl(level, o * wide + (threadIdx.x & 48));
@@ -535,8 +539,8 @@ __device__ __forceinline__ Choice route_four(const RouteView& g, const RouteLane
         bool kept = real;
         if (g.top_groups < g.groups) {
             // the same with the groups' words: the last one that is kept, and the first that is not
-            const float level = two && second != none ? first + second : first, half = two ? 0.5f : 1.f;
-            const float u = fmaf(level, unit * half, fmaf(two ? -2.f * low : -low, unit * half, 2.f));
+            const float level = two && second != none ? level_of(first, second) : first, half = two ? 0.5f : 1.f;
+            const float u = fmaf(level, unit * half, offset);          // (for two, half the steps of a range twice as wide)
             const uint32_t word = real ? (uint32_t)fmaxf(u, 0.f) << 5 | (16u - l.mine) : 0u;
             uint32_t in = 0x80000000u;
             for (int i = 0; i < g.top_groups; ++i) in += row_most(word - in);

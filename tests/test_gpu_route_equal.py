@@ -111,3 +111,20 @@ def test_all_equal(ctx, experts):
         for top_k in (1, 8, 14, 15, 31):
             for kw in (dict(), dict(bias=torch.zeros(experts)), dict(score="sigmoid", bias=torch.full((experts,), 0.5)), dict(score="sigmoid", groups=4, top_groups=4, group_top=2)):
                 check(ctx, x, top_k, **kw)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_top", [1, 2])
+@pytest.mark.parametrize("experts,groups,top_groups,top_k", [(20, 4, 1, 4), (12, 3, 1, 1), (64, 16, 3, 2), (8, 8, 5, 4), (256, 16, 9, 7), (600, 20, 3, 5), (60, 3, 1, 16)])
+def test_groups_and_biases_near_the_ends_of_fp32(ctx, experts, groups, top_groups, top_k, group_top, score):
+    """Groups are compared by sums that fp32 does not hold."""
+    g = torch.Generator().manual_seed(experts)
+    x = torch.randn((20, experts), generator=g)
+    kw = dict(score=score, groups=groups, top_groups=top_groups, group_top=group_top)
+    for mask in (torch.finfo(F32).min, -2e38):
+        for part in (0.3, 0.5, 0.9):
+            check(ctx, x, top_k, bias=torch.where(torch.rand(experts, generator=g) < part, mask, 0.0), **kw)
+    # (far enough from each other that the scores, which fp32 and 64 bits lose beside them, decide nothing)
+    ends = torch.tensor([-3.4e38, -2.5e38, -2e38, -1.1e38, -1e38, 0.0, 1e38, 1.4e38, 3.3e38])
+    for lo, hi in ((0, 6), (0, 9), (5, 9)):
+        check(ctx, x, top_k, bias=ends[torch.randint(lo, hi, (experts,), generator=g)], **kw)
