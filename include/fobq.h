@@ -572,7 +572,7 @@ int fobq_debug_offset_tables(int32_t k, int32_t pad, int64_t h, int64_t w, int32
  *   FOBQ_PLAN_ROUTE  in: tokens, experts
  *                  out: workgroups that have a part of the tokens each, tokens of a part, bytes of work
  *   FOBQ_PLAN_EXPERTS  in: compute units, packed rows, experts, rows of B, columns, type of the result (fobq_float), rows of B to a scale
- *                  out: packed rows and rows of B of a tile, workgroups
+ *                  out: packed rows and rows of B of a tile, workgroups, and, if asked for, sets of wavefronts that deal a tile's columns
  *   FOBQ_PLAN_NORM_CHECK  in: rows, cols, x_ld, residual_ld, sum_ld, norm_ld, type, weight_type, sign of an eps that is wrong (-1: below 0, 1: Inf; 0: 1e-6), then addresses
  *                  (not followed) of X, residual, weight, sum, norm
  *                  out: what a call says of such a norm (fobq_status)

@@ -112,12 +112,13 @@ int experts_debug_plan(int32_t what, const int64_t* in, int32_t n_in, int64_t* o
         out[0] = p.parts; out[1] = p.per_part; out[2] = route_workspace(p, (int)in[1]);
         return FOBQ_OK;
     }
-    if (what == FOBQ_PLAN_EXPERTS && n_in == 7 && n_out == 3) {
+    if (what == FOBQ_PLAN_EXPERTS && n_in == 7 && (n_out == 3 || n_out == 4)) {
         for (int i = 0; i < 5; ++i)
             if (in[i] < (i ? 0 : 16) || in[i] > (i ? i == 2 ? MAX_EXPERTS : MAX_ROWS : 4096)) return FOBQ_EINVAL;
         if (in[2] < 1 || !is_float((int)in[5]) || (in[6] != 1 && in[6] != 128)) return FOBQ_EINVAL;
         const ExpertPlan p = expert_plan((int)in[0], in[1], (int)in[2], in[3], in[4], (int)in[5], (int)in[6]);
         out[0] = p.tm; out[1] = p.tn; out[2] = p.tiles;
+        if (n_out == 4) out[3] = p.parts;
         return FOBQ_OK;
     }
     if (what == FOBQ_PLAN_NORM_CHECK && n_in == 14 && n_out == 1) {
