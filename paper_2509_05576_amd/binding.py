@@ -799,8 +799,8 @@ def _dense(t: torch.Tensor, ctx: int, dtype: torch.dtype, shape, what: str) -> i
 def fobq_route(ctx: int, logits: torch.Tensor, top_k: int, *, score: str = "softmax", bias: Optional[torch.Tensor] = None, groups: int = 1, top_groups: int = 1,
                group_top: int = 2, renormalize: bool = True, scale: float = 1.0, out: Optional[Routing] = None) -> Routing:
     """logits (fp32, bf16 or fp16, tokens x experts) -> the top_k experts of each token and their weights.  score: "softmax" or "sigmoid"; bias (fp32, experts): added for
-    the choice, not for the weights; groups: only the top_groups groups of neighbouring experts are chosen from, which count as the sum of their group_top
-    (1 or 2) best; renormalize: the weights are relative to the sum of the chosen ones; scale: times the weights.  No gradient passes it."""
+    the choice, not for the weights (-inf: never chosen, which is faster than other large negative values); groups: only the top_groups groups of neighbouring
+    experts are chosen from, which count as the sum of their group_top (1 or 2) best; renormalize: the weights are relative to the sum of the chosen ones; scale: times the weights.  No gradient passes it."""
     _need(logits, ctx, _FLOAT, 2, "logits")
     tokens, experts = logits.shape
     if score not in _SCORES:

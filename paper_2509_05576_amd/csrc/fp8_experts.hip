@@ -116,8 +116,8 @@ __device__ __forceinline__ void copy16_from(const uint8_t* src, void* lds_base)
 }
 
 // TM x TN outputs by WM x WN wavefronts, the tiles of STAGES - 1 blocks under way.  FA, FB: the types of A and B; PER: rows of B to a scale.
-// (32768 rows in 64 experts of 4096 x 2048, bf16, a scale per 128 x 128: 376 us, 1.46 PFLOP/s, in tiles of 256 x 256; with 512 rows in each expert 345, as one
-// product of as many rows in whole tiles takes 302.  A tile's 16 blocks take 32 us, its start and end 6, of which the stores 4.7; a block's products alone take
+// (32768 rows in 64 experts of 4096 x 2048, bf16, a scale per 128 x 128: 376 to 390 us, 1.41 to 1.46 PFLOP/s, in tiles of 256 x 256; with 512 packed rows in each expert 316, as one
+// product of as many rows in whole tiles takes 299.  A tile's 16 blocks take 32 us, its start and end 6, of which the stores 4.7; a block's products alone take
 // 1.47, its copies alone 1.71: LDS has both.  256 rows in 128 experts of 2048 x 2048: 80 us, 5.4 TB/s.)
 // With PARTS above 1 as many such sets of wavefronts deal the blocks of columns among them, and add up in LDS, in their order.
 template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, int FA, int FB, int PER, bool EXACT>
@@ -144,8 +144,8 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS) void fp8_experts_kernel(Exper
     // Rows of A behind the tile's last are that one again, and not stored; rows of B behind its last read as zeros.
     // The copies of the block that is fetched stand between the products of the one that is multiplied, a few to each of the first 1 / SPREAD of its groups: all in front of
     // them, the first operands wait until the addresses of all are through.  With two stages they have to be under way by the middle, or the next block waits
-    // for them.  (32768 rows in 64 experts of 4096 x 2048: 386 -> 376 us, with a scale per row, 128 x 256, 480 -> 459; 1400 rows in 8 of 1024 x 4096 21.9 -> 20.0.  On fp16
-    // values, whose order is the compiler's, 427 -> 560: not there.)
+    // for them.  (Both in turn, four times: 32768 rows in 64 experts of 4096 x 2048 391 -> 386 us, no more than a run differs from the next; with a scale per row, 128 x 256, 477 -> 454;
+    // 16384 rows in 64 of 1024 x 2048 71.5 -> 65.8; 1400 rows in 8 of 1024 x 4096 20.0 -> 18.7.  On fp16 values, whose order is the compiler's, 427 -> 560: not there.)
     constexpr int SPREAD = PARTS > 1 || EXACT ? 0 : STAGES == 2 ? 2 : 1;
     constexpr int PA = TM * 8 / THREADS, PB = TN * 8 / THREADS, STEP = THREADS / 8;
     static_assert(TM % STEP == 0 && TN % STEP == 0 && STEP % 16 == 0, "pieces of whole rows, the same place in each");
@@ -465,8 +465,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_experts_few_kernel(ExpertV
 //   16, 64 x 64, 64 x 128    1 token to 2 of 8 experts of 4096 x 4096: 9.6, 12.3, 13.1; 8 to 3 of 7 of 1000 x 2304: 7.2, 8.3, 8.8; 32: 10.2, 8.4, 10.3;
 //                            8 to 4 of 64 of 1024 x 2048: 15.6, 11.4, 11.2; 32 to 8 of 128 of 2048 x 2048: 132, 84, 80 (memory)
 //   64 x 64, 64 x 128        7 experts of 1000 x 2304, 143 rows: 12.6, 13.6; 439 rows: 23.3, 18.8
-//   64 x 64, its blocks dealt to two sets of wavefronts   7 experts of 1000 x 2304, 14, 55 and 143 rows: 8.4, 10.0, 12.6 with one, 8.3, 9.6, 13.2 with two (fp32 and a
-//                            scale per row: 11.6, 15.1, 22.3 and 10.4, 13.3, 20.2); 4 of 3000 x 1000, 83 rows: 9.1 and 10.2
+//   64 x 64, its blocks dealt to one set of wavefronts, to two   bf16, 7 experts of 1000 x k, 14 rows, k 1024, 1536, 2304, 4096: 5.7, 6.7, 8.1, 11.4 and 6.0, 6.8, 7.9, 10.7; 8 of
+//                            1024 x k, 64 rows, k 1024, 1536, 2048, 2304: 6.9, 8.0, 9.2, 9.8 and 6.9, 7.9, 8.9, 9.4 (k 4096: no difference); more tiles than compute units,
+//                            4 of 3000 x k, 83 rows, k 1024, 2304, 4096: 8.0, 12.3, 18.0 and 8.8, 13.4, 19.0; fp32 and a scale per row, 7 of 1000 x k, 143 rows, k 512,
+//                            1024, 1536, 2304: 9.0, 13.0, 16.4, 21.4 and 10.5, 12.9, 15.5, 19.6; 8 of 1024 x k, 64 rows, k 512, 1024, 2304: 7.3, 9.7, 15.3 and 7.5, 9.3, 13.3
 //   64 x 128, 128 x 256, 256 x 256   64 experts of 4096 x 2048, 128 rows: 181, 150, 176; 512 rows: 530, 410, 381; 8 of 4096 x 4096, 83 rows: 29, 35, 45;
 //                            256 rows: 64, 69, 58; 1024 rows: 219, 181, 178; 64 of 1024 x 2048, 256 rows: 71, 63, 66
 //   fp32, 64 x 128, 128 x 128, 128 x 256   8 of 4096 x 4096, 1024 rows: 365, 321, 352; 128 of 2048 x 2048, 64 rows: 168, 170, 166

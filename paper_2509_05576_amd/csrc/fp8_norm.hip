@@ -148,7 +148,7 @@ __device__ __forceinline__ float swiglu(float gate, float up)
     return gate * r * up;
 }
 
-// Eight lanes have a block, whichever row it is in.  (bf16, 32768 x 2048: 71 us, 4.7 TB/s; with 36 instructions a value instead of 25 it was bound by them, 92.)
+// Eight lanes have a block, whichever row it is in.  (bf16, 32768 x 2048: 69 to 73 us, 4.6 to 4.9 TB/s; fp32 113, 5.3; with 36 instructions a value instead of 25 it was bound by them, 92.)
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void swiglu_kernel(const T* __restrict__ x, int64_t ld, Fp8View out)
 {

@@ -320,7 +320,8 @@ __device__ __forceinline__ Choice route_token(const RouteView& g, const RouteLan
         got = choose<V>(logit, g, l, 0.f, logit, sure);
     } else {
         // In fp32 first.  A score is off by less than 40 units of the largest one, the sum with a bias by one unit of either more: keys that are
-        // apart by more than twice that are in the order that 64 bits have.  Tokens with nearer ones (some in a thousand) are looked at in 64 bits.
+        // apart by more than twice that are in the order that 64 bits have.  Tokens with nearer ones (some in a thousand; nearly all of them beside finite biases far from the
+        // others, as masks of -1e9) are looked at in 64 bits.
         float key[V], total = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -738,8 +739,9 @@ __device__ __forceinline__ void route_places(RouteShared& sh, const RouteView& g
 }
 
 // All of it where one workgroup has the tokens; otherwise the choice, and how often each expert is in it.  Bound by the vector instructions of the choice, not by memory:
-// 16384 tokens x 256 fp32 logits take 15 to 18 us (17 MB, 4 us of a copy); alone, 64 tokens x 128 take 7.7 us, 64 x 256 with a bias and groups 12.6.  One workgroup for
-// more than 64 tokens saves a launch (65 x 128: 9.9 -> 8.8) but has fewer wavefronts (128 x 128: 9.9 -> 11.7,
+// 16384 tokens x 256 fp32 logits take 16 to 20 us (17 MB, 4 us of a copy); alone, 64 tokens x 128 take 7.4 us, 64 x 256 with a bias and groups 12.8.  Of that, looking
+// at equals beside the last choice is 0.3 to 1.5 us (16384 x 128, bf16, whose logits are often equal: 13.1 -> 14.1 with the places; in steps of 1/4: 13.6 -> 15.3).
+// One workgroup for more than 64 tokens saves a launch (65 x 128: 9.9 -> 8.8) but has fewer wavefronts (128 x 128: 9.9 -> 11.7,
 // 192 x 128: 10.2 -> 15.5): two launches from there on.
 template <class T, int V, bool SCORED, bool FOUR>
 __global__ __launch_bounds__(64 * ROUTE_WAVES) void route_choose_kernel(RouteView g, RoutePlan p, int32_t* __restrict__ work)
